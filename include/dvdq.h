@@ -295,6 +295,100 @@ int dvdq_gbs_reset(void *state, int initial_bits, void *hip_stream);
 int dvdq_gbs_step(const void *f_t_bf16, const void *f_prev_bf16, int64_t n, float delta, int b_low, int b_high,
                   void *state, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * What a model runs around its quantized layers: rotary positions of the projections' outputs, the products that stay in 16
+ * bits, with their epilogue, and the group norm of the video decoder.
+ *
+ * Conventions as above, but for these: tensors are DVDQ_BF16, DVDQ_FP16 or (where said) DVDQ_FP32, all tensors of a call of one type;
+ * they are views with strides, counted in elements, whose last dimension is dense; their addresses need only be those of an element
+ * (DVDQ_ERR_ALIGN otherwise), workspaces and tables 16 bytes.  An output may be the input (or residual) itself, at the same address
+ * with the same strides; other overlaps are the caller's to avoid.  Strides of an output may not be 0 over a dimension above 1, and an output
+ * that is an input may not have other strides (DVDQ_ERR_UNSUPPORTED).  A call over nothing (no batches, no tokens) does nothing and
+ * returns DVDQ_OK.  NaN and infinities spread as in the formulas.
+ */
+enum { DVDQ_BF16 = 0, DVDQ_FP16 = 1, DVDQ_FP32 = 2 };
+enum { DVDQ_ACT_NONE = 0, DVDQ_ACT_SILU = 1, DVDQ_ACT_GELU_TANH = 2, DVDQ_ACT_GELU = 3 };
+
+/*
+ * Rotary positions.  With R = rot_dim and (c, s) = table[positions[b, t, axis(j)], j], every pair j = 0 .. R/2 - 1 of every head becomes
+ *
+ *     (a, b) -> (a c - b s, a s + b c)           DVDQ_ROPE_INVERSE: (a c + b s, b c - a s)
+ *
+ * where the pair is elements j and j + R/2 of the head, or 2j and 2j + 1 with DVDQ_ROPE_INTERLEAVED; elements from R on are
+ * copied.  The inverse takes a rotation back (table of magnitude 1), and is the rotation's backward pass: gradients of the outputs in,
+ * gradients of the inputs out.
+ *
+ *   q, k           the heads to rotate, [B, T, heads, head_dim] with the given strides; k may be NULL.  Type as `dtype`, any of the three
+ *   table     in   fp32 [n_pos, R/2, 2]: cosine and sine of every position and pair (dvdq_rope_table)
+ *   positions in   int32 [B, T, n_axes], batches `pos_batch` elements apart (0: one row for all).  A negative position leaves its
+ *                  pairs as they are (text tokens beside video tokens); one of n_pos or more makes them NaN
+ *   sections       host, n_axes even numbers that add up to R: the part of the rotated elements that each axis turns (t, h, w of a
+ *                  video); pairs belong to the axes in order.  May be NULL for one axis
+ *
+ * Limits: head_dim at most 1024, n_axes 1 to 4, B T at most 2^23 (DVDQ_ERR_UNSUPPORTED).  2 <= R <= head_dim, even (DVDQ_ERR_SHAPE).
+ */
+typedef struct {
+    const void *in;
+    void *out;
+    int64_t heads;
+    int64_t in_stride[3], out_stride[3];   /* batch, token, head */
+} dvdq_rope_heads;
+enum { DVDQ_ROPE_INTERLEAVED = 1, DVDQ_ROPE_INVERSE = 2 };
+int dvdq_rope(const dvdq_rope_heads *q, const dvdq_rope_heads *k, int64_t B, int64_t T, int64_t head_dim, const float *table,
+              int64_t n_pos, int64_t rot_dim, const int32_t *positions, int64_t pos_batch, int n_axes, const int32_t *sections,
+              int flags, int dtype, void *hip_stream);
+
+/*
+ * One-time, offline: the table of dvdq_rope.  table[p, j] = magnitude * (cos(p * freq[j]), sin(p * freq[j])), in fp64, rounded once.
+ *   freq   in   fp64 [half], device: the angle per position of every pair.  Frequencies stretched for longer contexts than a model
+ *               was trained on are the caller's to compute (a model's handful of numbers); `magnitude` is for schemes that scale the
+ *               products of queries and keys with them
+ *   table  out  fp32 [n_pos, half, 2]
+ * n_pos, half >= 1 (DVDQ_ERR_SHAPE); half at most 512, n_pos * half at most 2^31 (DVDQ_ERR_UNSUPPORTED).
+ */
+int dvdq_rope_table(const double *freq, int64_t n_pos, int64_t half, double magnitude, float *table, void *hip_stream);
+
+/*
+ * Matrix product of 16-bit activations and weights with its epilogue:
+ *
+ *     y[m, n] = residual[m, n] + gate[m / (M / gate_rows), n] * act(sum_k x[m, k] w[n, k] + bias[n])
+ *
+ * summed and finished in fp32, rounded once.  DVDQ_BF16 or DVDQ_FP16 (DVDQ_ERR_UNSUPPORTED otherwise).
+ *   x         in   [M, K], rows ldx elements apart
+ *   w         in   [N, K], rows ldw apart
+ *   bias      in   [N] or NULL
+ *   act            one of DVDQ_ACT_*
+ *   gate      in   [gate_rows, N], rows ldg apart, or NULL; gate_rows divides M: each row is for M / gate_rows consecutive tokens
+ *   residual  in   [M, N], rows ldr apart, or NULL; may be y
+ *   y         out  [M, N], rows ldy apart
+ *   workspace      device, 16-byte aligned, at least dvdq_linear_workspace_bytes(M, N, K) (which may be 0: then NULL will do).
+ *                  Scratch: calls that may run at the same time need one each
+ * M >= 0, N, K >= 1, pitches no less than a row (DVDQ_ERR_SHAPE); M at most 2^23, N and K at most 2^22 (DVDQ_ERR_UNSUPPORTED).  The order of
+ * summation is fixed by the arguments: results do not change from call to call.
+ */
+int dvdq_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias, int act, const void *gate,
+                int64_t gate_rows, int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype, void *y,
+                int64_t ldy, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t dvdq_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
+/*
+ * Group norm with an activation, channels last:
+ *
+ *     y[b, s, c] = act((x[b, s, c] - mean[b, g]) / sqrt(var[b, g] + eps) * weight[c] + bias[c]),   g = c / (C / groups)
+ *
+ * with mean and biased variance over the S rows (all positions of a frame or clip) and C / groups channels of the group; statistics
+ * and arithmetic in fp32 or more, rounded once.
+ *   x, y           [B, S, C]: batches x_batch, rows x_row elements apart; any of the three types; y may be x
+ *   weight, bias   [C] or NULL, of the same type
+ *   act            DVDQ_ACT_NONE or DVDQ_ACT_SILU (DVDQ_ERR_UNSUPPORTED otherwise)
+ *   workspace      device, 16-byte aligned, at least dvdq_group_norm_workspace_bytes(B, S, C, groups); scratch, as above
+ * groups >= 1 divides C; eps >= 0; rows no closer than C (DVDQ_ERR_SHAPE).  C at most 4096, B at most 65535 (DVDQ_ERR_UNSUPPORTED).
+ */
+int dvdq_group_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_batch, int64_t x_row, int64_t groups,
+                    const void *weight, const void *bias, float eps, int act, int dtype, void *y, int64_t y_batch, int64_t y_row,
+                    void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t dvdq_group_norm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t groups);
+
 const char *dvdq_status_string(int status);
 int dvdq_version(void);
 

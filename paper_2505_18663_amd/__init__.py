@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import ctypes as C
 import importlib.util
+import math
 import os
 import sys
 import warnings
@@ -23,19 +24,23 @@ import torch
 __all__ = [
     "DvdqError", "DvdqLibraryMissing", "lib", "library_path", "version", "status_string",
     "rotate_quant", "rotate_quant_blockwise", "w4ax_gemm", "qlinear", "qlinear_static", "static_workspace_bytes", "qlinear_workspace_bytes", "qlinear_scale_offset", "qlinear_rowsum_offset", "workspace_rowsum",
-    "w4_prepack", "w4_native_bytes", "w4_prepack_fp6", "w4_native_fp6_bytes", "codes_bytes", "bgr_quantize", "GbsController", "bench_copy", "bench_mfma_i8", "bench_mfma_fp6", "bench_set_gemm_variant", "bench_set_gemm_schedule", "bench_fill_tile_counters", "bench_set_gemm_grid_limit", "release_stream",
+    "w4_prepack", "w4_native_bytes", "w4_prepack_fp6", "w4_native_fp6_bytes", "codes_bytes", "bgr_quantize", "GbsController",
+    "rope_frequencies", "rope_table", "rope", "linear", "linear_workspace_bytes", "group_norm", "group_norm_workspace_bytes",
+    "ACT_NONE", "ACT_SILU", "ACT_GELU_TANH", "ACT_GELU", "bench_copy", "bench_mfma_i8", "bench_mfma_fp6", "bench_set_gemm_variant", "bench_set_gemm_schedule", "bench_fill_tile_counters", "bench_set_gemm_grid_limit", "release_stream",
     "W_CANONICAL", "W_NATIVE", "W_NATIVE_FP6", "CODES_INT8", "CODES_PACKED4", "CODES_FP6", "BGR_LISTING", "BGR_BEST_OF_ALL", "EXPORTED_SYMBOLS",
 ]
 
 W_CANONICAL, W_NATIVE, W_NATIVE_FP6 = 0, 1, 2
 CODES_INT8, CODES_PACKED4, CODES_FP6 = 0, 1, 2
 BGR_LISTING, BGR_BEST_OF_ALL = 0, 1
+ACT_NONE, ACT_SILU, ACT_GELU_TANH, ACT_GELU = 0, 1, 2, 3
 
 EXPORTED_SYMBOLS = (
     "dvdq_rotate_quant", "dvdq_rotate_quant_blockwise", "dvdq_w4ax_gemm", "dvdq_qlinear", "dvdq_qlinear_workspace_bytes",
     "dvdq_qlinear_scale_offset", "dvdq_qlinear_rowsum_offset", "dvdq_qlinear_static", "dvdq_static_workspace_bytes", "dvdq_w4_prepack", "dvdq_w4_native_bytes", "dvdq_w4_prepack_fp6",
     "dvdq_w4_native_fp6_bytes", "dvdq_codes_bytes", "dvdq_status_string",
-    "dvdq_version", "dvdq_gbs_workspace_bytes", "dvdq_gbs_reset", "dvdq_gbs_step", "dvdq_bgr_quantize", "dvdq_bench_copy", "dvdq_bench_mfma_i8", "dvdq_bench_mfma_fp6", "dvdq_bench_set_gemm_variant", "dvdq_bench_set_gemm_schedule", "dvdq_bench_fill_tile_counters", "dvdq_bench_set_gemm_grid_limit", "dvdq_bench_set_gbs_wait", "dvdq_bench_gemm_choice", "dvdq_bench_narrow_tiles", "dvdq_bench_quantizer_waves", "dvdq_bench_qlinear_choice", "dvdq_bench_bgr_choice", "dvdq_release_stream",
+    "dvdq_version", "dvdq_rope", "dvdq_rope_table", "dvdq_linear", "dvdq_linear_workspace_bytes", "dvdq_group_norm", "dvdq_group_norm_workspace_bytes",
+    "dvdq_gbs_workspace_bytes", "dvdq_gbs_reset", "dvdq_gbs_step", "dvdq_bgr_quantize", "dvdq_bench_copy", "dvdq_bench_mfma_i8", "dvdq_bench_mfma_fp6", "dvdq_bench_set_gemm_variant", "dvdq_bench_set_gemm_schedule", "dvdq_bench_fill_tile_counters", "dvdq_bench_set_gemm_grid_limit", "dvdq_bench_set_gbs_wait", "dvdq_bench_gemm_choice", "dvdq_bench_narrow_tiles", "dvdq_bench_quantizer_waves", "dvdq_bench_qlinear_choice", "dvdq_bench_bgr_choice", "dvdq_release_stream",
 )
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -53,6 +58,11 @@ class DvdqError(RuntimeError):
 
 class DvdqLibraryMissing(RuntimeError):
     pass
+
+
+class _RopeHeads(C.Structure):
+    """dvdq_rope_heads"""
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("heads", C.c_int64), ("in_stride", C.c_int64 * 3), ("out_stride", C.c_int64 * 3)]
 
 
 class _Handback:
@@ -122,6 +132,18 @@ def lib() -> C.CDLL:
     L.dvdq_gbs_step.restype = i32
     L.dvdq_bgr_quantize.argtypes = [vp, i64, i64, i32, i32, C.c_double, i32, vp, vp, vp, vp, vp]
     L.dvdq_bgr_quantize.restype = i32
+    L.dvdq_rope.argtypes = [C.POINTER(_RopeHeads), C.POINTER(_RopeHeads), i64, i64, i64, vp, i64, i64, vp, i64, i32, C.POINTER(C.c_int32), i32, i32, vp]
+    L.dvdq_rope.restype = i32
+    L.dvdq_rope_table.argtypes = [vp, i64, i64, C.c_double, vp, vp]
+    L.dvdq_rope_table.restype = i32
+    L.dvdq_linear.argtypes = [vp, i64, vp, i64, vp, i32, vp, i64, i64, vp, i64, i64, i64, i64, i32, vp, i64, vp, sz, vp]
+    L.dvdq_linear.restype = i32
+    L.dvdq_linear_workspace_bytes.argtypes = [i64, i64, i64]
+    L.dvdq_linear_workspace_bytes.restype = sz
+    L.dvdq_group_norm.argtypes = [vp, i64, i64, i64, i64, i64, i64, vp, vp, C.c_float, i32, i32, vp, i64, i64, vp, sz, vp]
+    L.dvdq_group_norm.restype = i32
+    L.dvdq_group_norm_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    L.dvdq_group_norm_workspace_bytes.restype = sz
     L.dvdq_bench_copy.argtypes = [vp, vp, sz, vp]
     L.dvdq_bench_mfma_i8.argtypes = [i32, i32, vp, C.POINTER(C.c_double), vp]
     L.dvdq_bench_mfma_fp6.argtypes = [i32, i32, vp, C.POINTER(C.c_double), vp]
@@ -514,6 +536,223 @@ class GbsController:
 
     def bits(self) -> int:
         return self.read()[2]
+
+
+# ------------------------------------------------------------------ around the quantized layer
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _need_view(t, dtype, shape, name, device=None):
+    """A view with any strides whose last dimension is dense."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name}: expected a CUDA/HIP tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name}: expected dtype {dtype}, got {t.dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: expected device {device}, got {t.device}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dim() and t.size(-1) > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension must be dense")
+    return t
+
+
+def _workspace(workspace, need, device):
+    """The given workspace, or a new one where one is needed; and its size."""
+    if workspace is None:
+        workspace = torch.empty((need,), dtype=torch.uint8, device=device) if need else None
+    else:
+        _need(workspace, torch.uint8, None, "workspace")
+    return workspace, 0 if workspace is None else workspace.numel()
+
+
+def rope_frequencies(rot_dim, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: int = 0,
+                     beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """(angles per position of every rotated pair, magnitude of the rotation), host numbers for rope_table.
+
+    rot_dim: rotated elements of a head, or a sequence of them, one per axis: pair i of an axis with R elements turns by
+    base ** (-2 i / R) per position.  `scaling` stretches them by `factor` for contexts longer than the `original_length` positions
+    a model was trained on:
+      "linear"  positions are divided by the factor
+      "ntk"     the base grows by factor ** (R / (R - 2)): the slowest pair is stretched by the factor, the fastest not at all
+      "yarn"    pairs that turn more than `beta_fast` times within the original length stay, those that turn less than `beta_slow` times
+                are divided by the factor, a linear ramp over the pair's number in between; magnitude 1 + 0.1 ln(factor)"""
+    parts = [int(rot_dim)] if isinstance(rot_dim, int) else [int(r) for r in rot_dim]
+    if not parts or any(r < 0 or r % 2 for r in parts) or sum(parts) < 2:
+        raise ValueError("rot_dim: expected even numbers")
+    if scaling not in ("none", "linear", "ntk", "yarn"):
+        raise ValueError(f"scaling: unknown scheme {scaling!r}")
+    if not base > 1.0 or not factor >= 1.0:
+        raise ValueError("base must be above 1 and factor at least 1")
+    if scaling == "yarn" and not (original_length >= 1 and beta_fast > beta_slow > 0):
+        raise ValueError("yarn: needs original_length >= 1 and beta_fast > beta_slow > 0")
+    freq = []
+    for R in parts:
+        b = base * factor ** (R / (R - 2)) if scaling == "ntk" and R > 2 else base
+        f = [b ** (-2.0 * i / R) for i in range(R // 2)]
+        if scaling == "linear":
+            f = [v / factor for v in f]
+        elif scaling == "yarn" and R:
+            # the (real) number of the pair that turns `n` times within the original length
+            pair = lambda n: R * math.log(original_length / (n * 2.0 * math.pi)) / (2.0 * math.log(base))   # noqa: E731
+            low = min(max(math.floor(pair(beta_fast)), 0), R - 1)
+            high = min(max(math.ceil(pair(beta_slow)), 0), R - 1)
+            for i, v in enumerate(f):
+                ramp = min(max((i - low) / max(high - low, 1e-3), 0.0), 1.0)
+                f[i] = v * (1.0 - ramp) + v / factor * ramp
+        freq += f
+    return freq, (1.0 + 0.1 * math.log(factor) if scaling == "yarn" else 1.0)
+
+
+def rope_table(n_pos: int, freq, magnitude: float = 1.0, device="cuda", table=None, stream=None):
+    """Table of cosines and sines for `rope`, made once per model: fp32 [n_pos, len(freq), 2].  freq: angle per position of every
+    pair (rope_frequencies, or a model's own), a sequence of numbers or an fp64 tensor on the GPU.  See dvdq_rope_table."""
+    L = lib()
+    if not isinstance(freq, torch.Tensor):
+        freq = torch.tensor(freq, dtype=torch.float64, device=device if table is None else table.device)
+    _need(freq, torch.float64, None, "freq")
+    shape = (n_pos, freq.numel(), 2)
+    if table is None:
+        table = torch.empty(shape, dtype=torch.float32, device=freq.device)
+    _need(table, torch.float32, shape, "table")
+    _check(L.dvdq_rope_table(_ptr(freq), n_pos, freq.numel(), float(magnitude), _ptr(table), _stream(stream)), "dvdq_rope_table")
+    return table
+
+
+def _rope_heads(x, out, D, name, dtype, lead):
+    _need_view(x, dtype, None, name)
+    if x.dim() != len(lead) + 2 or tuple(x.shape[:-2]) != lead or x.size(-1) != D:
+        raise ValueError(f"{name}: expected shape {lead + ('heads', D)}, got {tuple(x.shape)}")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _need_view(out, x.dtype, x.shape, name + "_out", x.device)
+    st = [(0,) * (4 - t.dim()) + t.stride()[:-1] for t in (x, out)]
+    return out, _RopeHeads(_ptr(x), _ptr(out), x.size(-2), (C.c_int64 * 3)(*st[0]), (C.c_int64 * 3)(*st[1]))
+
+
+def rope(q, k, table, positions, sections=None, interleaved: bool = False, inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """Rotary positions of q and k (k may be None): [tokens, heads, D] or [batch, tokens, heads, D] views with any strides (of a fused
+    projection's output, or transposed from [batch, heads, tokens, D]).  table: fp32 [n_pos, R/2, 2] (rope_table).  positions: int32
+    [tokens] or [batch, tokens]; with sections (rotated elements per axis), [..., axes].  A negative position leaves its pairs as they
+    are.  q_out, k_out: where to, e.g. q and k themselves; new dense tensors otherwise.  inverse: the opposite angle, which is the
+    backward pass.  Returns (q_out, k_out), or q_out alone without k.  See dvdq_rope."""
+    L = lib()
+    _need_view(q, None, None, "q")
+    if q.dtype not in _DTYPES:
+        raise TypeError(f"q: expected bfloat16, float16 or float32, got {q.dtype}")
+    if q.dim() not in (3, 4):
+        raise ValueError("q: expected [tokens, heads, D] or [batch, tokens, heads, D]")
+    lead, D = tuple(q.shape[:-2]), q.size(-1)
+    B, T = (1,) * (2 - len(lead)) + lead
+    _need(table, torch.float32, None, "table")
+    if table.dim() != 3 or table.size(2) != 2:
+        raise ValueError("table: expected shape [n_pos, R/2, 2]")
+    _need(positions, torch.int32, None, "positions")
+    axes = () if sections is None else (len(sections),)
+    if tuple(positions.shape) == (T,) + axes:
+        pos_batch = 0
+    elif tuple(positions.shape) == (B, T) + axes:
+        pos_batch = T * (axes[0] if axes else 1) if B > 1 else 0
+    else:
+        raise ValueError(f"positions: expected shape {(T,) + axes} or {(B, T) + axes}, got {tuple(positions.shape)}")
+    q_out, hq = _rope_heads(q, q_out, D, "q", q.dtype, lead)
+    if k is not None:
+        k_out, hk = _rope_heads(k, k_out, D, "k", q.dtype, lead)
+    for name, t in (("k", k), ("table", table), ("positions", positions)):
+        if t is not None and t.device != q.device:
+            raise ValueError(f"{name}: expected device {q.device}, got {t.device}")
+    sec = None if sections is None else (C.c_int32 * len(sections))(*sections)
+    _check(L.dvdq_rope(C.byref(hq), None if k is None else C.byref(hk), B, T, D, _ptr(table), table.size(0), 2 * table.size(1),
+                       _ptr(positions), pos_batch, axes[0] if axes else 1, sec, (1 if interleaved else 0) | (2 if inverse else 0),
+                       _DTYPES[q.dtype], _stream(stream)), "dvdq_rope")
+    return q_out if k is None else (q_out, k_out)
+
+
+def linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return lib().dvdq_linear_workspace_bytes(M, N, K)
+
+
+def linear(x, w, bias=None, act: int = ACT_NONE, gate=None, residual=None, y=None, workspace=None, stream=None):
+    """y = residual + gate * act(x w^T + bias) in 16 bits (bf16 or fp16), summed and finished in fp32, rounded once.  x: [M, K], w:
+    [N, K], both with rows of any pitch; bias [N]; gate [N] or [G, N], a row for each M / G consecutive tokens; residual [M, N], which
+    y may be.  Returns y [M, N].  See dvdq_linear."""
+    L = lib()
+    _need_view(x, None, None, "x")
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise TypeError(f"x: expected bfloat16 or float16, got {x.dtype}")
+    if x.dim() != 2:
+        raise ValueError("x: expected shape [M, K]")
+    M, K = x.shape
+    _need_view(w, x.dtype, None, "w", x.device)
+    if w.dim() != 2 or w.size(1) != K:
+        raise ValueError(f"w: expected shape [N, {K}], got {tuple(w.shape)}")
+    N = w.size(0)
+    if bias is not None:
+        _need_view(bias, x.dtype, (N,), "bias", x.device)
+    gate_rows = 0
+    if gate is not None:
+        _need_view(gate, x.dtype, None, "gate", x.device)
+        gate_rows = 1 if gate.dim() == 1 else gate.size(0)
+        if gate.dim() not in (1, 2) or gate.size(-1) != N:
+            raise ValueError(f"gate: expected shape [{N}] or [G, {N}], got {tuple(gate.shape)}")
+    if residual is not None:
+        _need_view(residual, x.dtype, (M, N), "residual", x.device)
+    if y is None:
+        y = torch.empty((M, N), dtype=x.dtype, device=x.device)
+    else:
+        _need_view(y, x.dtype, (M, N), "y", x.device)
+    workspace, n_ws = _workspace(workspace, L.dvdq_linear_workspace_bytes(M, N, K), x.device)
+    _check(L.dvdq_linear(_ptr(x), x.stride(0), _ptr(w), w.stride(0), _ptr(bias), int(act), _ptr(gate), gate_rows,
+                         gate.stride(0) if gate_rows > 1 else N, _ptr(residual), 0 if residual is None else residual.stride(0), M, N, K,
+                         _DTYPES[x.dtype], _ptr(y), y.stride(0), _ptr(workspace), n_ws, _stream(stream)), "dvdq_linear")
+    return y
+
+
+def group_norm_workspace_bytes(B: int, S: int, C: int, groups: int) -> int:
+    return lib().dvdq_group_norm_workspace_bytes(B, S, C, groups)
+
+
+def _rows_of(t, name):
+    """(rows of a batch, elements between batches, between rows) of a [B, ..., C] view; the dimensions in between must lie in order."""
+    rows, step, below = 1, t.size(-1), None
+    for n, st in zip(reversed(t.shape[1:-1]), reversed(t.stride()[1:-1])):
+        if n == 1:
+            continue
+        if below is None:
+            step = st
+        elif st != below:
+            raise ValueError(f"{name}: the dimensions between batch and channels must be those of one sequence of rows")
+        rows, below = rows * n, st * n
+    return rows, t.stride(0), step
+
+
+def group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, act: int = ACT_NONE, y=None, workspace=None, stream=None):
+    """y = act(group norm of x), channels last: x [B, ..., C] (bf16, fp16 or fp32; a channels-last module's tensor as
+    x.movedim(1, -1)), statistics over the dimensions in between and each of `groups` runs of channels; weight and bias [C] of the same
+    type; act ACT_NONE or ACT_SILU; y may be x.  Returns y.  See dvdq_group_norm."""
+    L = lib()
+    _need_view(x, None, None, "x")
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"x: expected bfloat16, float16 or float32, got {x.dtype}")
+    if x.dim() < 2:
+        raise ValueError("x: expected shape [B, ..., C]")
+    B, n_ch = x.size(0), x.size(-1)
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None:
+            _need_view(t, x.dtype, (n_ch,), name, x.device)
+    if y is None:
+        y = torch.empty_like(x)
+        if n_ch > 1 and y.stride(-1) != 1:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _need_view(y, x.dtype, x.shape, "y", x.device)
+    S, x_batch, x_row = _rows_of(x, "x")
+    _, y_batch, y_row = _rows_of(y, "y")
+    workspace, n_ws = _workspace(workspace, L.dvdq_group_norm_workspace_bytes(B, S, n_ch, groups), x.device)
+    _check(L.dvdq_group_norm(_ptr(x), B, S, n_ch, x_batch, x_row, int(groups), _ptr(weight), _ptr(bias), float(eps), int(act),
+                             _DTYPES[x.dtype], _ptr(y), y_batch, y_row, _ptr(workspace), n_ws, _stream(stream)), "dvdq_group_norm")
+    return y
 
 
 # ------------------------------------------------------------------ calibration helpers

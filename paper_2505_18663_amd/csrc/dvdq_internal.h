@@ -160,6 +160,20 @@ int bgr_choice(int64_t N, int64_t K, int n_steps, int max_refine);   // threads 
 int launch_bgr(const float *w, int64_t N, int64_t K, int n_steps, int max_refine, double eps, int search,
                uint8_t *w_packed, float *w_scale, int8_t *w_zero, double *row_error, hipStream_t stream);
 
+// Around the quantized layer (rope.hip, linear16.hip, group_norm.hip); arguments as in the C ABI, validated in api_model.hip
+int launch_rope_table(const double *freq, int64_t n_pos, int64_t half, double magnitude, float *table, hipStream_t stream);
+int launch_rope(const dvdq_rope_heads *q, const dvdq_rope_heads *k, int64_t B, int64_t T, int64_t D, const float *table, int64_t n_pos,
+                int64_t R, const int32_t *positions, int64_t pos_batch, int n_axes, const int32_t *sections, bool interleaved, bool inverse,
+                int dtype, hipStream_t stream);
+size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias, int act, const void *gate, int64_t gate_rows,
+                  int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype, void *y, int64_t ldy,
+                  void *workspace, hipStream_t stream);
+size_t group_norm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t groups);
+int launch_group_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_batch, int64_t x_row, int64_t groups, const void *weight,
+                      const void *bias, float eps, int act, int dtype, void *y, int64_t y_batch, int64_t y_row, void *workspace,
+                      hipStream_t stream);
+
 // Raise a kernel's dynamic-LDS limit to `bytes` once per kernel and device (`done` is the call
 // site's own bit mask of devices already configured).  Not a stream operation: after the first
 // launch on a device nothing but the launch itself is issued, also under stream capture.

@@ -1,0 +1,225 @@
+// Group norm with an activation, channels last:
+//
+//   y[b, s, c] = act((x[b, s, c] - mean[b, g]) / sqrt(var[b, g] + eps) * weight[c] + bias[c]),   g = c / (C / groups)
+//
+// mean and var (biased) over the S rows and the C / groups channels of a group.  Every few rows of a channel are summed up, then their
+// squared deviations from their own mean, and parts are joined by count, mean and sum of squared deviations: channels far from zero
+// and rows unlike the others lose nothing (differences to a value picked beforehand do, where that value is such a row's).
+#include "elem.h"
+#include "wave_reduce.h"
+
+namespace dvdq {
+
+namespace {
+
+struct Moments { float mean, m2; };   // of a part of a group: mean, sum of squared deviations from it
+
+struct GnArgs {
+    const void *x;
+    void *y;
+    const void *weight, *bias;
+    int64_t x_batch, x_row, y_batch, y_row;   // elements between batches, rows
+    int64_t S;
+    int C, groups, cpg;
+    int cols, rows_at_once;                   // pieces of a row; rows a workgroup takes at once
+    int64_t slab_rows;                        // rows of a part
+    int slabs;
+    float eps;
+    Moments *parts;                           // [B][slabs][groups]
+    float2 *stats;                            // [B][groups]: mean, 1 / sqrt(var + eps)
+};
+
+// Joins the moments of `nb` values to those of `n`, for every channel of a piece.
+template <int V>
+static __device__ __forceinline__ void join(float n, float (&mean)[V], float (&m2)[V], float nb, const float (&meanb)[V], const float (&m2b)[V]) {
+    const float share = nb / (n + nb), weight = n * share;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float d = meanb[i] - mean[i];
+        mean[i] = fmaf(d, share, mean[i]);
+        m2[i] += fmaf(d * d, weight, m2b[i]);
+    }
+}
+
+constexpr int kBatch = 8;   // rows of a thread that are in registers at a time
+
+template <typename E>
+__global__ __launch_bounds__(1024) void gn_parts(GnArgs a) {
+    using Raw = typename E::Raw;
+    constexpr int V = E::kVec;
+    extern __shared__ float lds[];                      // [rows_at_once][2][cols * V]
+    const int b = blockIdx.y, slab = blockIdx.x;
+    const int64_t s0 = slab * a.slab_rows;
+    const int rows = (int)min(a.S - s0, a.slab_rows);
+    const int width = a.cols * V;
+    const int r = threadIdx.x / a.cols, col = threadIdx.x - r * a.cols, c0 = col * V, n = min(V, a.C - c0);
+    const int64_t step = a.rows_at_once * a.x_row;
+    if (r < a.rows_at_once) {
+        const Raw *x = static_cast<const Raw *>(a.x) + (b * a.x_batch + (s0 + r) * a.x_row + c0);
+        const int mine = (rows - r + a.rows_at_once - 1) / a.rows_at_once;   // rows of this thread (0 or less: none)
+        float mean[V] = {}, m2[V] = {};
+        for (int i0 = 0; i0 < mine; i0 += kBatch) {
+            const int nb = min(kBatch, mine - i0);
+            Piece<E> p[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (i < nb) p[i] = load_piece<E>(x + i * step, n);
+                else p[i] = Piece<E>{};
+            x += kBatch * step;
+            // (differences to the first row: a constant channel has no deviations at all, whatever the rounding of 1 / nb)
+            float mb[V] = {}, qb[V] = {};
+#pragma unroll
+            for (int i = 1; i < kBatch; ++i)
+                if (i < nb) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) mb[j] += E::to_f32(p[i].e[j]) - E::to_f32(p[0].e[j]);
+                }
+            const float inv = 1.0f / (float)nb;
+#pragma unroll
+            for (int j = 0; j < V; ++j) mb[j] = fmaf(mb[j], inv, E::to_f32(p[0].e[j]));
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (i < nb) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float d = E::to_f32(p[i].e[j]) - mb[j];
+                        qb[j] = fmaf(d, d, qb[j]);
+                    }
+                }
+            join<V>((float)i0, mean, m2, (float)nb, mb, qb);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            lds[(2 * r) * width + c0 + j] = mean[j];
+            lds[(2 * r + 1) * width + c0 + j] = m2[j];
+        }
+    }
+    __syncthreads();
+    // per channel: mean and squared deviations over the slab, in the first two rows of lds
+    for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+        const float first = lds[c];
+        float sum = 0.0f, m2 = 0.0f;
+        for (int i = 1; i < a.rows_at_once; ++i) sum = fmaf((float)max(0, (rows - i + a.rows_at_once - 1) / a.rows_at_once), lds[2 * i * width + c] - first, sum);
+        const float mean = first + sum / (float)rows;
+        for (int i = 0; i < a.rows_at_once; ++i) {
+            const float d = lds[2 * i * width + c] - mean;
+            m2 += fmaf((float)max(0, (rows - i + a.rows_at_once - 1) / a.rows_at_once), d * d, lds[(2 * i + 1) * width + c]);
+        }
+        lds[c] = mean;
+        lds[width + c] = m2;
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    for (int g = wave; g < a.groups; g += waves) {
+        float sum = 0.0f, m2 = 0.0f;
+        const float first = lds[g * a.cpg];
+        for (int c = lane; c < a.cpg; c += 64) sum += lds[g * a.cpg + c] - first;
+        const float mean = first + wave_sum(sum) / (float)a.cpg;
+        for (int c = lane; c < a.cpg; c += 64) {
+            const float d = lds[g * a.cpg + c] - mean;
+            m2 += fmaf((float)rows * d, d, lds[width + g * a.cpg + c]);
+        }
+        m2 = wave_sum(m2);
+        if (lane == 0) a.parts[((int64_t)b * a.slabs + slab) * a.groups + g] = {mean, m2};
+    }
+}
+
+// A wave joins the parts of one group of one batch.
+__global__ __launch_bounds__(64) void gn_join(GnArgs a) {
+    const int g = blockIdx.x, b = blockIdx.y;
+    const Moments *p = a.parts + (int64_t)b * a.slabs * a.groups + g;
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < a.slabs; i += 64) {
+        const int64_t rows = min(a.S - i * a.slab_rows, a.slab_rows);
+        sum += (double)rows * p[(int64_t)i * a.groups].mean;
+    }
+    const double mean = wave_sum(sum) / (double)a.S;
+    double m2 = 0.0;
+    for (int i = threadIdx.x; i < a.slabs; i += 64) {
+        const int64_t rows = min(a.S - i * a.slab_rows, a.slab_rows);
+        const Moments m = p[(int64_t)i * a.groups];
+        const double d = (double)m.mean - mean;
+        m2 += m.m2 + (double)(rows * a.cpg) * d * d;
+    }
+    const double var = wave_sum(m2) / ((double)a.S * a.cpg);
+    if (threadIdx.x == 0) a.stats[b * a.groups + g] = make_float2((float)mean, (float)(1.0 / sqrt(var + (double)a.eps)));
+}
+
+template <typename E, int ACT>
+__global__ __launch_bounds__(1024) void gn_apply(GnArgs a) {
+    using Raw = typename E::Raw;
+    constexpr int V = E::kVec;
+    const int b = blockIdx.y;
+    const int r = threadIdx.x / a.cols, col = threadIdx.x - r * a.cols, c0 = col * V, n = min(V, a.C - c0);
+    if (r >= a.rows_at_once) return;
+    float mean[V], scale[V], shift[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int c = min(c0 + i, a.C - 1);
+        const float2 st = a.stats[b * a.groups + c / a.cpg];
+        mean[i] = st.x;
+        scale[i] = st.y * (a.weight ? E::to_f32(static_cast<const Raw *>(a.weight)[c]) : 1.0f);
+        shift[i] = a.bias ? E::to_f32(static_cast<const Raw *>(a.bias)[c]) : 0.0f;
+    }
+    const Raw *x = static_cast<const Raw *>(a.x) + b * a.x_batch + c0;
+    Raw *y = static_cast<Raw *>(a.y) + b * a.y_batch + c0;
+    const int64_t s0 = blockIdx.x * a.slab_rows, s1 = min(a.S, s0 + a.slab_rows);
+    for (int64_t s = s0 + r; s < s1; s += a.rows_at_once) {
+        Piece<E> p = load_piece<E>(x + s * a.x_row, n);
+#pragma unroll
+        for (int i = 0; i < V; ++i) p.e[i] = E::from_f32(activate<ACT>(fmaf(E::to_f32(p.e[i]) - mean[i], scale[i], shift[i])));
+        store_piece<E>(y + s * a.y_row, p, n);
+    }
+}
+
+struct Plan { int cols, rows_at_once, threads, slabs; int64_t slab_rows; size_t parts_bytes, stats_bytes; };
+
+Plan plan(int64_t B, int64_t S, int64_t C, int64_t groups, int vec) {
+    Plan p;
+    p.cols = (int)((C + vec - 1) / vec);
+    p.threads = p.cols <= 256 ? 256 : (p.cols + 63) / 64 * 64;
+    p.rows_at_once = p.threads / p.cols;
+    const int64_t want = max((int64_t)1, (int64_t)2048 / B);                              // workgroups to fill the chip
+    p.slab_rows = max((S + want - 1) / want, (int64_t)8 * p.rows_at_once);
+    p.slab_rows = (p.slab_rows + p.rows_at_once - 1) / p.rows_at_once * p.rows_at_once;
+    p.slabs = (int)((S + p.slab_rows - 1) / p.slab_rows);
+    p.parts_bytes = ((size_t)B * p.slabs * groups * sizeof(Moments) + 255) / 256 * 256;
+    p.stats_bytes = ((size_t)B * groups * sizeof(float2) + 255) / 256 * 256;
+    return p;
+}
+
+}  // namespace
+
+size_t group_norm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t groups) {
+    size_t most = 0;
+    for (int vec : {4, 8}) {
+        const Plan p = plan(B, S, C, groups, vec);
+        most = max(most, p.parts_bytes + p.stats_bytes);
+    }
+    return most;
+}
+
+int launch_group_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_batch, int64_t x_row, int64_t groups, const void *weight,
+                      const void *bias, float eps, int act, int dtype, void *y, int64_t y_batch, int64_t y_row, void *workspace,
+                      hipStream_t stream) {
+    return with_type(dtype, [&](auto type) {
+        using E = decltype(type);
+        const Plan p = plan(B, S, C, groups, E::kVec);
+        GnArgs a = {};
+        a.x = x, a.y = y, a.weight = weight, a.bias = bias;
+        a.x_batch = x_batch, a.x_row = x_row, a.y_batch = y_batch, a.y_row = y_row;
+        a.S = S, a.C = (int)C, a.groups = (int)groups, a.cpg = (int)(C / groups);
+        a.cols = p.cols, a.rows_at_once = p.rows_at_once, a.slab_rows = p.slab_rows, a.slabs = p.slabs;
+        a.eps = eps;
+        a.parts = static_cast<Moments *>(workspace);
+        a.stats = reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) + p.parts_bytes);
+        const dim3 grid(p.slabs, (unsigned)B);
+        gn_parts<E><<<grid, p.threads, (size_t)p.rows_at_once * 2 * p.cols * E::kVec * sizeof(float), stream>>>(a);
+        gn_join<<<dim3((unsigned)groups, (unsigned)B), 64, 0, stream>>>(a);
+        if (act == DVDQ_ACT_SILU) gn_apply<E, DVDQ_ACT_SILU><<<grid, p.threads, 0, stream>>>(a);
+        else gn_apply<E, DVDQ_ACT_NONE><<<grid, p.threads, 0, stream>>>(a);
+        return check_launch();
+    });
+}
+
+}  // namespace dvdq
