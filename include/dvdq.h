@@ -363,7 +363,8 @@ int dvdq_rope_table(const double *freq, int64_t n_pos, int64_t half, double magn
  *   y         out  [M, N], rows ldy apart
  *   workspace      device, 16-byte aligned, at least dvdq_linear_workspace_bytes(M, N, K) (which may be 0: then NULL will do).
  *                  Scratch: calls that may run at the same time need one each
- * M >= 0, N, K >= 1, pitches no less than a row (DVDQ_ERR_SHAPE); M at most 2^23, N and K at most 2^22 (DVDQ_ERR_UNSUPPORTED).  The order of
+ * M >= 0, N, K >= 1, pitches no less than a row (DVDQ_ERR_SHAPE); M at most 2^23, N and K at most 2^22, ldy and ldr at most 2^26
+ * (DVDQ_ERR_UNSUPPORTED).  The order of
  * summation is fixed by the arguments: results do not change from call to call.
  */
 int dvdq_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias, int act, const void *gate,

@@ -4,7 +4,7 @@
 namespace {
 
 constexpr int64_t kMaxInt = 0x7FFFFFFF;
-constexpr int64_t kMaxTokens = (int64_t)1 << 23, kMaxChannels = (int64_t)1 << 22;   // what a launch's grid and 32-bit indices hold
+constexpr int64_t kMaxTokens = (int64_t)1 << 23, kMaxChannels = (int64_t)1 << 22, kMaxPitch = (int64_t)1 << 26;   // what a launch's grid and 32-bit indices hold
 
 inline bool aligned_to(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline size_t element_bytes(int dtype) { return dtype == DVDQ_FP32 ? 4 : 2; }
@@ -80,7 +80,7 @@ int dvdq_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const vo
     if ((M > 1 && (ldx < K || ldy < N || (residual && ldr < N))) || (N > 1 && ldw < K) || (gate && gate_rows > 1 && ldg < N))
         return DVDQ_ERR_SHAPE;
     if (M > kMaxTokens || N > kMaxChannels || K > kMaxChannels || act < DVDQ_ACT_NONE || act > DVDQ_ACT_GELU || (dtype != DVDQ_BF16 && dtype != DVDQ_FP16) ||
-        (residual == y && M > 1 && ldr != ldy))
+        (residual == y && M > 1 && ldr != ldy) || (M > 1 && (ldy > kMaxPitch || (residual && ldr > kMaxPitch))))
         return DVDQ_ERR_UNSUPPORTED;
     for (const void *p : {x, w, bias, gate, residual, static_cast<const void *>(y)})
         if (!aligned_to(p, 2)) return DVDQ_ERR_ALIGN;

@@ -1,6 +1,8 @@
 // Element types of the operators around the quantized layer (rope.hip, group_norm.hip, linear16.hip): conversions to and from
 // fp32, 16-byte pieces of a row at any element's address, activations.
 #pragma once
+#include <type_traits>
+
 #include "dvdq_internal.h"
 
 namespace dvdq {
@@ -74,6 +76,17 @@ inline int with_type(int dtype, F f) {
         case DVDQ_BF16: return f(Bf16());
         case DVDQ_FP16: return f(Fp16());
         default: return f(Fp32());
+    }
+}
+
+// The same for an activation.
+template <class F>
+inline int with_act(int act, F f) {
+    switch (act) {
+        case DVDQ_ACT_SILU: return f(std::integral_constant<int, DVDQ_ACT_SILU>());
+        case DVDQ_ACT_GELU_TANH: return f(std::integral_constant<int, DVDQ_ACT_GELU_TANH>());
+        case DVDQ_ACT_GELU: return f(std::integral_constant<int, DVDQ_ACT_GELU>());
+        default: return f(std::integral_constant<int, DVDQ_ACT_NONE>());
     }
 }
 

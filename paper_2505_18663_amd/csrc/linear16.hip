@@ -28,72 +28,102 @@ struct LinearArgs {
     int64_t ldx, ldw, ldr, ldy, ldg;   // elements between rows
     int M, N, K;
     int gate_rows;                     // tokens of one row of the gate
-    int act;
 };
 
-// Bias, activation, gate, residual and store of 8 consecutive channels of a token.
-template <typename E, int ACT>
-static __device__ __forceinline__ void finish(const LinearArgs &a, float (&v)[8], const float (&bias)[8], int m, int n, int count) {
+// What follows the sums of a wave's 64 channels x 16 FM tokens, from channel n0 of token m0 on: the lane's token of fragment j is
+// m0 + 16 j + lane % 16, its channels 8 (lane / 16) .. + 7 and the same 32 further on (channel_of_row).
+template <typename E, int ACT, int FM>
+static __device__ __forceinline__ void epilogue(const LinearArgs &a, const v4f (&acc)[4][FM], int m0, int n0) {
+    constexpr int B = FM < 4 ? FM : 4;
+    const int lane = threadIdx.x & 63, row = lane & 15, col = 8 * (lane >> 4);
+    if (m0 >= a.M || n0 >= a.N) return;
+    const bool shared_gate = a.gate && m0 / a.gate_rows == (min(m0 + 16 * FM, a.M) - 1) / a.gate_rows;   // one row for all tokens
+    const uint32_t off_y = row * (uint32_t)a.ldy + col, off_r = row * (uint32_t)a.ldr + col;             // elements
+    uint16_t *y = const_cast<uint16_t *>(uniform_ptr(a.y + (m0 * a.ldy + n0)));
+    const uint16_t *res = a.residual ? uniform_ptr(a.residual + (m0 * a.ldr + n0)) : nullptr;
+    auto values = [&](float (&v)[8], int h, int j, const Piece<E> &bias) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = activate<ACT>(v[i] + bias[i]);
-    if (a.gate) {
-        const Piece<E> p = load_piece<E>(a.gate + (m / a.gate_rows) * a.ldg + n, count);
+        for (int i = 0; i < 8; ++i) v[i] = activate<ACT>(acc[2 * h + i / 4][j][i & 3] + E::to_f32(bias.e[i]));
+    };
+    auto times = [](float (&v)[8], const Piece<E> &p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= E::to_f32(p.e[i]);
-    }
-    if (a.residual) {
-        const Piece<E> p = load_piece<E>(a.residual + m * a.ldr + n, count);
+    };
+    auto plus = [](float (&v)[8], const Piece<E> &p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += E::to_f32(p.e[i]);
-    }
-    Piece<E> o;
+    };
+    auto rounded = [](const float (&v)[8]) {
+        Piece<E> o;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.e[i] = E::from_f32(v[i]);
-    store_piece<E>(a.y + m * a.ldy + n, o, count);
-}
-
-// A wave's 64 channels x 16 FM tokens: the lane's token of fragment j is m + 16 j, its channels n .. n + 15 (channel_of_row).
-template <typename E, int ACT, int FM>
-static __device__ __forceinline__ void finish_tile(const LinearArgs &a, v4f (&acc)[4][FM], int m, int n) {
+        for (int i = 0; i < 8; ++i) o.e[i] = E::from_f32(v[i]);
+        return o;
+    };
+    if (m0 + 16 * FM <= a.M && n0 + 64 <= a.N) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int count = min(8, a.N - n - 8 * h);
-        if (count <= 0) return;
-        float bias[8] = {};
-        if (a.bias) {
-            const Piece<E> p = load_piece<E>(a.bias + n + 8 * h, count);
+        for (int h = 0; h < 2; ++h) {
+            const int n = n0 + 32 * h + col;
+            Piece<E> bias = {}, gate;
+            if (a.bias) bias = load_piece<E>(a.bias + n, 8);
+            if (shared_gate) gate = load_piece<E>(a.gate + (m0 / a.gate_rows) * a.ldg + n, 8);
+            // the residual of B tokens is on its way while the B before are worked off (y may be the residual: the compiler could not
+            // move a load above a store)
+            Piece<E> r[2][B];
+            auto fetch = [&](int j0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) bias[i] = E::to_f32(p.e[i]);
+                for (int j = 0; j < B; ++j) r[(j0 / B) & 1][j] = load_piece<E>(res + 16 * (j0 + j) * a.ldr + 32 * h + off_r, 8);
+            };
+            if (res) fetch(0);
+#pragma unroll
+            for (int j0 = 0; j0 < FM; j0 += B) {
+                if (j0 + B < FM && res) fetch(j0 + B);
+#pragma unroll
+                for (int j = 0; j < B; ++j) {
+                    float v[8];
+                    values(v, h, j0 + j, bias);
+                    if (a.gate) {
+                        if (!shared_gate) gate = load_piece<E>(a.gate + ((m0 + 16 * (j0 + j) + row) / a.gate_rows) * a.ldg + n, 8);
+                        times(v, gate);
+                    }
+                    if (res) plus(v, r[(j0 / B) & 1][j]);
+                    store_piece<E>(y + 16 * (j0 + j) * a.ldy + 32 * h + off_y, rounded(v), 8);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
         }
+    } else {
 #pragma unroll
-        for (int j = 0; j < FM; ++j) {
-            if (m + 16 * j >= a.M) break;
-            float v[8];
+        for (int h = 0; h < 2; ++h) {
+            const int n = n0 + 32 * h + col, count = min(8, a.N - n);
+            Piece<E> bias = {};
+            if (a.bias && count > 0) bias = load_piece<E>(a.bias + n, count);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = acc[2 * h + i / 4][j][i & 3];
-            finish<E, ACT>(a, v, bias, m + 16 * j, n + 8 * h, count);
+            for (int j = 0; j < FM; ++j) {
+                const int m = m0 + 16 * j + row;
+                if (m < a.M && count > 0) {
+                    float v[8];
+                    values(v, h, j, bias);
+                    if (a.gate) times(v, load_piece<E>(a.gate + (m / a.gate_rows) * a.ldg + n, count));
+                    if (res) plus(v, load_piece<E>(res + 16 * j * a.ldr + 32 * h + off_r, count));
+                    store_piece<E>(y + 16 * j * a.ldy + 32 * h + off_y, rounded(v), count);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-    }
-}
-template <typename E, int FM>
-static __device__ __forceinline__ void epilogue(const LinearArgs &a, v4f (&acc)[4][FM], int m, int n) {
-    switch (a.act) {
-        case DVDQ_ACT_SILU: finish_tile<E, DVDQ_ACT_SILU>(a, acc, m, n); break;
-        case DVDQ_ACT_GELU_TANH: finish_tile<E, DVDQ_ACT_GELU_TANH>(a, acc, m, n); break;
-        case DVDQ_ACT_GELU: finish_tile<E, DVDQ_ACT_GELU>(a, acc, m, n); break;
-        default: finish_tile<E, DVDQ_ACT_NONE>(a, acc, m, n);
     }
 }
 
 // The weights are the matrix instruction's rows, the tokens its columns, so that a lane's four results are four channels of one
-// token.  Row r of fragment f of 64 channels is channel 16 (r / 4) + 4 f + r % 4: over the four fragments a lane then holds 16
-// consecutive channels of a token, and the four lanes of a token 64, which are stored without a detour.
-static __device__ __forceinline__ int channel_of_row(int row) { return (row & ~63) + 16 * ((row & 15) >> 2) + 4 * ((row & 63) >> 4) + (row & 3); }
+// token.  Row r of fragment f of 64 channels is channel 32 (f / 2) + 8 (r / 4) + 4 (f % 2) + r % 4: two fragments are then 8
+// consecutive channels of a lane, 16 bytes, and the four lanes of a token store 64 bytes in a row, without a detour.
+static __device__ __forceinline__ int channel_of_row(int row) {
+    return (row & ~63) + 32 * ((row >> 5) & 1) + 8 * ((row & 15) >> 2) + 4 * ((row >> 4) & 1) + (row & 3);
+}
 
 // Any sizes, pitches and addresses: 128 x 128 outputs of four waves, 64 x 64 each, operands through registers into LDS rows of 64
 // elements of K.  The 16-byte pieces of an LDS row are permuted by its row number, so that the 16 rows that a read takes at once
 // lie in different banks.
-template <typename E>
+template <typename E, int ACT>
 __global__ __launch_bounds__(256) void linear_any(LinearArgs a) {
     constexpr int BK = 64;
     __shared__ uint4 lds_w[128 * 8], lds_x[128 * 8];
@@ -136,7 +166,7 @@ __global__ __launch_bounds__(256) void linear_any(LinearArgs a) {
                 for (int j = 0; j < 4; ++j) acc[i][j] = mfma<E>(fw[i], fx[j], acc[i][j]);
         }
     }
-    epilogue<E>(a, acc, m0 + wm + (lane & 15), n0 + wn + 16 * (lane >> 4));
+    epilogue<E, ACT>(a, acc, __builtin_amdgcn_readfirstlane(m0 + wm), __builtin_amdgcn_readfirstlane(n0 + wn));
 }
 
 // ---- rows of whole 16-byte pieces: operands straight into LDS
@@ -149,119 +179,171 @@ static __device__ __forceinline__ void lds_direct_load16_at(const void *p, uint3
 
 __device__ uint4 zero_piece;   // what the pieces past K of the last slice are read from
 
-// Tiles of 64 WN channels x 16 FM WM tokens, WN x WM waves of 64 channels x 16 FM tokens each; slices of 64 elements of K, two of
-// them in LDS.  A slice is worked off in phases of 16 (or fewer) matrix instructions, and a phase begins by requesting the fragments
-// of the next one, so that the matrix cores have operands when it ends.  Before the last phase of a slice, whose fragments
-// are then in registers, stands the slice's one barrier: behind it the next slice is in LDS for every wave, and the buffer of this one is free for
-// the slice after that.
-template <typename E, int FM, int WN, int WM>
-__global__ __launch_bounds__(64 * WN * WM, FM * WN * WM == 64 ? 2 : 2) void linear_tiles(LinearArgs a) {
+// Tiles of 64 WN channels x 16 FM WM tokens, WN x WM waves of 64 channels x 16 FM tokens each; slices of 64 elements of K.
+// Weights have three slices in LDS, tokens two: while a slice is multiplied, the next is there, the weights of the one after it
+// come in, and its tokens follow as soon as those of the present slice have been read.  (What bounds the loop on a full chip is the way from
+// the L2s into LDS, 55 to 65 GB/s per compute unit where 32 of them share panels; it must not run dry.)
+// A slice is worked off in phases of 16 matrix instructions (or fewer), and a phase begins by requesting the fragments of the next one.
+// Before the last phase of a slice, whose fragments are then in registers, stands the slice's one barrier: behind it the next slice is
+// in LDS for every wave, and this one's place is free.
+// A workgroup takes tile after tile, without a seam: the last slices of a tile load the first ones of the next, which is multiplied
+// while the outputs are still being written.
+template <typename E, int ACT, int FM, int WN, int WM>
+__global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, int group_n) {
     constexpr int W = WN * WM, BN = 64 * WN, BM = 16 * FM * WM, FH = FM < 4 ? FM : 4, NH = FM / FH, P = 2 * NH;
     constexpr int LW = BN / 8 / W, LX = BM / 8 / W;          // loads of a wave per slice, 8 rows each
-    constexpr uint32_t kBufBytes = (BN + BM) * 128;
-    extern __shared__ uint4 lds[];
+    constexpr int kStores = 2 * FM;                          // of a wave per whole tile
+    constexpr uint32_t kUnitW = BN * 128, kUnitX = BM * 128;
+    extern __shared__ uint4 lds[];                           // weights: 3 units, tokens: 2
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n_tiles = (a.N + BN - 1) / BN, m_tiles = (a.M + BM - 1) / BM;
-    int m0, n0;
-    {
-        // consecutive workgroups go to different XCDs: each XCD takes one run of tiles, 4 columns wide
-        const int total = gridDim.x, xcd = blockIdx.x & 7, i = blockIdx.x >> 3;
-        const int t = xcd * (total >> 3) + min(xcd, total & 7) + i;
-        tile_origin(t, m_tiles, n_tiles, 4, BM, BN, m0, n0);
-    }
+    const int n_tiles = (a.N + BN - 1) / BN, m_tiles = (a.M + BM - 1) / BM, tiles = n_tiles * m_tiles, grid = gridDim.x;
     const int wn = wave % WN * 64, wm = wave / WN * 16 * FM;
+    const int slices = max(2, (a.K + 63) >> 6);
 
-    const uint32_t lds0 = lds_address(lds);
-    const uint8_t *src_w = reinterpret_cast<const uint8_t *>(uniform_ptr(a.w + n0 * a.ldw));
-    const uint8_t *src_x = reinterpret_cast<const uint8_t *>(uniform_ptr(a.x + m0 * a.ldx));
+    // Consecutive workgroups go to different XCDs.  Each XCD has one run of tiles, which its workgroups take in order: those that run
+    // at the same time share panels, and so do those of the next round (as interleaved rounds of the whole chip, 32760 x 13824 x 5120
+    // took 3340 us in place of 3190).
+    const int xcds = min(8, grid), xcd = blockIdx.x % xcds, step = (grid - xcd + xcds - 1) / xcds;
+    const int end = (int)((int64_t)tiles * (xcd + 1) / xcds);
+    const uint32_t lds_w = lds_address(lds) + wave * (1024 * LW), lds_x = lds_address(lds) + 3 * kUnitW + wave * (1024 * LX);
+    const uint8_t *src_w, *src_x;
     uint32_t off_w[LW], off_x[LX];
+    int m0, n0;
+    auto aim = [&](int t) {                                  // the loads' source: tile t
+        tile_origin(t, m_tiles, n_tiles, group_n, BM, BN, m0, n0);
+        src_w = reinterpret_cast<const uint8_t *>(uniform_ptr(a.w + n0 * a.ldw));
+        src_x = reinterpret_cast<const uint8_t *>(uniform_ptr(a.x + m0 * a.ldx));
 #pragma unroll
-    for (int j = 0; j < LW; ++j) {
-        const int row = wave * (8 * LW) + 8 * j + (lane >> 3);
-        off_w[j] = (uint32_t)(min(channel_of_row(row), a.N - 1 - n0) * a.ldw * 2) + 16 * ((lane & 7) ^ ((row >> 1) & 7));
-    }
+        for (int j = 0; j < LW; ++j) {
+            const int row = wave * (8 * LW) + 8 * j + (lane >> 3);
+            off_w[j] = (uint32_t)(min(channel_of_row(row), a.N - 1 - n0) * a.ldw * 2) + 16 * ((lane & 7) ^ ((row >> 1) & 7));
+        }
 #pragma unroll
-    for (int j = 0; j < LX; ++j) {
-        const int row = wave * (8 * LX) + 8 * j + (lane >> 3);
-        off_x[j] = (uint32_t)(min(row, a.M - 1 - m0) * a.ldx * 2) + 16 * ((lane & 7) ^ ((row >> 1) & 7));
-    }
-    const int slices = (a.K + 63) >> 6;
-    auto load = [&](int q) {
-        const uint32_t to_w = lds0 + (q & 1) * kBufBytes + wave * (1024 * LW), to_x = lds0 + (q & 1) * kBufBytes + BN * 128 + wave * (1024 * LX);
-        const uint8_t *sw = src_w + (uint32_t)q * 128u, *sx = src_x + (uint32_t)q * 128u;
-        if ((q + 1) * 64 <= a.K) {
+        for (int j = 0; j < LX; ++j) {
+            const int row = wave * (8 * LX) + 8 * j + (lane >> 3);
+            off_x[j] = (uint32_t)(min(row, a.M - 1 - m0) * a.ldx * 2) + 16 * ((lane & 7) ^ ((row >> 1) & 7));
+        }
+    };
+    // slice q of the aimed tile; `whole`: known to lie within K
+    auto load_w = [&](int q, int slot, bool whole) {
+        const uint8_t *src = src_w + (uint32_t)q * 128u;
+        if (whole || (q + 1) * 64 <= a.K) {
 #pragma unroll
-            for (int j = 0; j < LW; ++j) lds_direct_load16(sw, off_w[j], to_w + 1024 * j);
-#pragma unroll
-            for (int j = 0; j < LX; ++j) lds_direct_load16(sx, off_x[j], to_x + 1024 * j);
+            for (int j = 0; j < LW; ++j) lds_direct_load16(src, off_w[j], lds_w + slot * kUnitW + 1024 * j);
         } else {
-            const uint32_t left = (uint32_t)(a.K - q * 64) * 2;   // bytes of a row that there are
 #pragma unroll
             for (int j = 0; j < LW; ++j) {
-                const uint32_t piece = 16 * ((lane & 7) ^ (((wave * (8 * LW) + 8 * j + (lane >> 3)) >> 1) & 7));
-                lds_direct_load16_at(piece < left ? static_cast<const void *>(sw + off_w[j]) : &zero_piece, to_w + 1024 * j);
+                const int piece = 16 * ((lane & 7) ^ (((wave * (8 * LW) + 8 * j + (lane >> 3)) >> 1) & 7));
+                lds_direct_load16_at(piece < (a.K - q * 64) * 2 ? static_cast<const void *>(src + off_w[j]) : &zero_piece, lds_w + slot * kUnitW + 1024 * j);
             }
+        }
+    };
+    auto load_x = [&](int q, int slot, bool whole) {
+        const uint8_t *src = src_x + (uint32_t)q * 128u;
+        if (whole || (q + 1) * 64 <= a.K) {
+#pragma unroll
+            for (int j = 0; j < LX; ++j) lds_direct_load16(src, off_x[j], lds_x + slot * kUnitX + 1024 * j);
+        } else {
 #pragma unroll
             for (int j = 0; j < LX; ++j) {
-                const uint32_t piece = 16 * ((lane & 7) ^ (((wave * (8 * LX) + 8 * j + (lane >> 3)) >> 1) & 7));
-                lds_direct_load16_at(piece < left ? static_cast<const void *>(sx + off_x[j]) : &zero_piece, to_x + 1024 * j);
+                const int piece = 16 * ((lane & 7) ^ (((wave * (8 * LX) + 8 * j + (lane >> 3)) >> 1) & 7));
+                lds_direct_load16_at(piece < (a.K - q * 64) * 2 ? static_cast<const void *>(src + off_x[j]) : &zero_piece, lds_x + slot * kUnitX + 1024 * j);
             }
         }
     };
 
-    // fragment reads: LDS row r of 128 bytes holds its 16-byte piece c at c ^ ((r >> 1) & 7)
+    // fragment reads: LDS row r of 128 bytes holds its 16-byte piece c at c ^ ((r >> 1) & 7), so that the 16 rows that a read takes at
+    // once lie in different banks
     const int at = (lane & 15) * 8 + ((lane >> 4) ^ ((lane & 15) >> 1));   // of k-step 0; k-step 1 is piece ^ 4
-    const int at_w = wn * 8 + at, at_x = BN * 8 + wm * 8 + at;
+    const int at_w = wn * 8 + at, at_x = 3 * (kUnitW / 16) + wm * 8 + at;
     v4f acc[4][FM] = {};
     uint4 fw[2][4], fx[2][FH];
-    auto read = [&](int buf, int p) {   // the fragments of phase p of the slice in `buf`
+    auto read = [&](int sw, int sx, int p) {                 // the fragments of phase p of the slice in these places
         const int ks = p / NH, h = p % NH;
-        const uint4 *base = lds + buf * (kBufBytes / 16);
         if (h == 0)
 #pragma unroll
-            for (int f = 0; f < 4; ++f) fw[ks][f] = base[(at_w ^ (4 * ks)) + 128 * f];
+            for (int f = 0; f < 4; ++f) fw[ks][f] = lds[sw * (kUnitW / 16) + (at_w ^ (4 * ks)) + 128 * f];
 #pragma unroll
-        for (int f = 0; f < FH; ++f) fx[p & 1][f] = base[(at_x ^ (4 * ks)) + 128 * (h * FH + f)];
+        for (int f = 0; f < FH; ++f) fx[p & 1][f] = lds[sx * (kUnitX / 16) + (at_x ^ (4 * ks)) + 128 * (h * FH + f)];
     };
 
-    load(0);
-    if (slices > 1) {
-        load(1);
-        wait_vmcnt<LW + LX>();
-    } else {
-        wait_vmcnt<0>();
-    }
+    int t = (int)((int64_t)tiles * xcd / xcds) + blockIdx.x / xcds, sw = 0, sx = 0;   // places of the present slice
+    if (t >= end) return;
+    aim(t);
+    load_w(0, 0, false);
+    load_x(0, 0, false);
+    load_w(1, 1, false);
+    load_x(1, 1, false);
+    wait_vmcnt<LW + LX>();
     asm volatile("s_barrier" ::: "memory");
-    read(0, 0);
-    for (int q = 0; q < slices; ++q) {
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-            if (p < P - 1) {
-                read(q & 1, p + 1);
-            } else if (q + 1 < slices) {
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                if (q + 2 < slices) load(q + 2);
-                read((q + 1) & 1, 0);
+    read(0, 0, 0);
+    bool stored = false;                                     // the outputs of a whole tile are on their way
+    while (true) {
+        const int cur_m = m0, cur_n = n0, next = t + step;
+        // STEADY: slices of this tile follow, all within K
+        auto slice = [&](int q, auto steady) {
+            constexpr bool STEADY = decltype(steady)::value;
+            const int nw = sw == 2 ? 0 : sw + 1, aw = nw == 2 ? 0 : nw + 1;
+            bool loads = true;                               // what is loaded two slices ahead
+            int lq = q + 2;
+            if (!STEADY && lq >= slices) {
+                lq -= slices;
+                loads = next < end;
+                if (lq == 0 && loads) aim(next);
             }
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int p = 0; p < P; ++p) {
+                if (p < P - 1) {
+                    read(sw, sx, p + 1);
+                    if (p == 0 && loads) load_w(lq, aw, STEADY);
+                } else if (STEADY || q + 1 < slices || next < end) {
+                    if (!STEADY && !loads) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    else if (STEADY || !(stored && q == 0)) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LW) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LW + kStores) : "memory");
+                    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                    if (loads) load_x(lq, sx, STEADY);
+                    if (STEADY || q + 1 < slices) read(nw, sx ^ 1, 0);   // (of the next tile: behind the outputs)
+                }
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int j = 0; j < FH; ++j) acc[i][(p % NH) * FH + j] = mfma<E>(fw[p / NH][i], fx[p & 1][j], acc[i][(p % NH) * FH + j]);
-            __builtin_amdgcn_sched_barrier(0);
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < FH; ++j) acc[i][(p % NH) * FH + j] = mfma<E>(fw[p / NH][i], fx[p & 1][j], acc[i][(p % NH) * FH + j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            sw = nw;
+            sx ^= 1;
+        };
+        const int steady = stored ? 1 : 0;
+#pragma unroll 1
+        for (int q = 0; q < slices; ++q) {
+            if (q == steady)
+                for (; q < slices - 3; ++q) slice(q, std::true_type());
+            slice(q, std::false_type());
         }
+        epilogue<E, ACT>(a, acc, cur_m + wm, cur_n + wn);
+        if (next >= end) return;
+        read(sw, sx, 0);
+        t = next;
+        stored = cur_m + BM <= a.M && cur_n + BN <= a.N;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j) acc[i][j] = v4f{};
     }
-    epilogue<E>(a, acc, m0 + wm + (lane & 15), n0 + wn + 16 * (lane >> 4));
 }
 
-template <typename E, int FM, int WN, int WM>
-int launch_tiles(const LinearArgs &a, hipStream_t stream) {
-    constexpr size_t kLds = 2 * (64 * WN + 16 * FM * WM) * 128;
+template <typename E, int ACT, int FM, int WN, int WM>
+int launch_tiles(const LinearArgs &a, int per_cu, hipStream_t stream) {
+    constexpr int BN = 64 * WN, BM = 16 * FM * WM;
+    constexpr size_t kLds = (3 * BN + 2 * BM) * 128;
     static std::atomic<uint64_t> done{0};
-    const auto kernel = linear_tiles<E, FM, WN, WM>;
+    const auto kernel = linear_tiles<E, ACT, FM, WN, WM>;
     allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kLds, done);
-    const unsigned tiles = (unsigned)((a.N + 64 * WN - 1) / (64 * WN)) * (unsigned)((a.M + 16 * FM * WM - 1) / (16 * FM * WM));
-    kernel<<<dim3(tiles), 64 * WN * WM, kLds, stream>>>(a);
+    const int n_tiles = (a.N + BN - 1) / BN, tiles = n_tiles * ((a.M + BM - 1) / BM);
+    // columns of tiles that are run through before the next row: panels of either side are shared by the workgroups of an XCD
+    const int groups = (n_tiles + 5) / 6;
+    kernel<<<dim3(min(tiles, 256 * per_cu)), 64 * WN * WM, kLds, stream>>>(a, (n_tiles + groups - 1) / groups);
     return check_launch();
 }
 
@@ -282,18 +364,20 @@ int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const 
     a.ldx = ldx, a.ldw = ldw, a.ldr = ldr, a.ldy = ldy, a.ldg = ldg;
     a.M = (int)M, a.N = (int)N, a.K = (int)K;
     a.gate_rows = gate ? (int)(M / gate_rows) : 1;
-    a.act = act;
     const auto whole = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 7) == 0 && ld < (int64_t)1 << 22; };
     const bool pieces = K % 8 == 0 && whole(x, M > 1 ? ldx : 0) && whole(w, N > 1 ? ldw : 0);
     return with_type(dtype, [&](auto type) {
         using E = decltype(type);
         if constexpr (sizeof(typename E::Raw) == 2) {
-            if (pieces) {
-                if (((M + 255) / 256) * ((N + 255) / 256) >= 256) return launch_tiles<E, 8, 4, 2>(a, stream);
-                return launch_tiles<E, 4, 2, 2>(a, stream);
-            }
-            linear_any<E><<<dim3((unsigned)(((N + 127) / 128) * ((M + 127) / 128))), 256, 0, stream>>>(a);
-            return check_launch();
+            return with_act(act, [&](auto which) {
+                constexpr int ACT = decltype(which)::value;
+                if (pieces) {
+                    if (((M + 255) / 256) * ((N + 255) / 256) >= 256) return launch_tiles<E, ACT, 8, 4, 2>(a, 1, stream);
+                    return launch_tiles<E, ACT, 4, 2, 2>(a, 2, stream);
+                }
+                linear_any<E, ACT><<<dim3((unsigned)(((N + 127) / 128) * ((M + 127) / 128))), 256, 0, stream>>>(a);
+                return check_launch();
+            });
         } else {
             return (int)DVDQ_ERR_UNSUPPORTED;
         }
