@@ -3,6 +3,8 @@
 //   y[m, n] = residual[m, n] + gate[m / (M / G), n] * act(sum_k x[m, k] w[n, k] + bias[n])
 //
 // Products on the matrix cores, sums and epilogue in fp32, one rounding to the tensors' type.
+#include <algorithm>
+
 #include "elem.h"
 #include "gemm_common.h"
 
@@ -28,7 +30,10 @@ struct LinearArgs {
     int64_t ldx, ldw, ldr, ldy, ldg;   // elements between rows
     int M, N, K;
     int gate_rows;                     // tokens of one row of the gate
+    float4 *parts;                     // sums of parts of K, in the order of the accumulators (kPart)
+    int splits, slices;                // parts of K; slices of 64 of a part
 };
+constexpr int kPart = 4;               // in the place of an activation: leave the sums of a part of K for linear_join
 
 // What follows the sums of a wave's 64 channels x 16 FM tokens, from channel n0 of token m0 on: the lane's token of fragment j is
 // m0 + 16 j + lane % 16, its channels 8 (lane / 16) .. + 7 and the same 32 further on (channel_of_row).
@@ -120,37 +125,50 @@ static __device__ __forceinline__ int channel_of_row(int row) {
     return (row & ~63) + 32 * ((row >> 5) & 1) + 8 * ((row & 15) >> 2) + 4 * ((row >> 4) & 1) + (row & 3);
 }
 
+// The sums of a wave, for linear_join: `at` numbers its fragments
+template <int FM>
+static __device__ __forceinline__ void store_part(const LinearArgs &a, const v4f (&acc)[4][FM], int64_t at) {
+#pragma unroll
+    for (int j = 0; j < FM; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.parts[((at + j) * 4 + i) * 64 + (threadIdx.x & 63)] = __builtin_bit_cast(float4, acc[i][j]);
+}
+
 // Any sizes, pitches and addresses: 128 x 128 outputs of four waves, 64 x 64 each, operands through registers into LDS rows of 64
-// elements of K.  The 16-byte pieces of an LDS row are permuted by its row number, so that the 16 rows that a read takes at once
-// lie in different banks.
+// elements of K, a slice ahead.  LDS as in linear_tiles.
 template <typename E, int ACT>
-__global__ __launch_bounds__(256) void linear_any(LinearArgs a) {
-    constexpr int BK = 64;
-    __shared__ uint4 lds_w[128 * 8], lds_x[128 * 8];
+__global__ __launch_bounds__(256, 2) void linear_any(LinearArgs a) {
+    extern __shared__ uint4 lds[];                           // two slices of 128 rows of weights, 128 of tokens
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n_tiles = (a.N + 127) / 128, tile_m = blockIdx.x / n_tiles;
-    const int n0 = (blockIdx.x - tile_m * n_tiles) * 128, m0 = tile_m * 128;
+    const int n_tiles = (a.N + 127) / 128, m_tiles = (a.M + 127) / 128, tiles = n_tiles * m_tiles;
+    const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
+    const int tile_m = tile / n_tiles;
+    const int n0 = (tile - tile_m * n_tiles) * 128, m0 = tile_m * 128;
     const int wn = (wave & 1) * 64, wm = (wave >> 1) * 64;
+    const int q0 = split * a.slices, q1 = min(q0 + a.slices, (a.K + 63) >> 6);
     v4f acc[4][4] = {};
     const int piece = tid & 7, row0 = tid >> 3;
-    for (int k0 = 0; k0 < a.K; k0 += BK) {
-        const int k = k0 + piece * 8, count = min(8, a.K - k);
-        Piece<E> pw[4], px[4];
+    Piece<E> pw[4], px[4];
+    auto load = [&](int q) {
+        const int k = q * 64 + piece * 8, count = min(8, a.K - k);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = row0 + 32 * i;
-            const int n = min(n0 + channel_of_row(row), a.N - 1), m = min(m0 + row, a.M - 1);
-            pw[i] = load_piece<E>(a.w + n * a.ldw + k, count);
-            px[i] = load_piece<E>(a.x + m * a.ldx + k, count);
+            pw[i] = load_piece<E>(a.w + min(n0 + channel_of_row(row), a.N - 1) * a.ldw + k, count);
+            px[i] = load_piece<E>(a.x + min(m0 + row, a.M - 1) * a.ldx + k, count);
         }
-        __syncthreads();
+    };
+    if (q0 < q1) load(q0);
+    for (int q = q0; q < q1; ++q) {
+        uint4 *lds_w = lds + (q & 1) * 2048, *lds_x = lds_w + 1024;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = row0 + 32 * i, at = row * 8 + (piece ^ ((row >> 1) & 7));
             lds_w[at] = __builtin_bit_cast(uint4, pw[i]);
             lds_x[at] = __builtin_bit_cast(uint4, px[i]);
         }
-        __syncthreads();
+        __syncthreads();                                     // (and every wave has read the slice before the last)
+        if (q + 1 < q1) load(q + 1);
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
             uint4 fw[4], fx[4];
@@ -166,7 +184,30 @@ __global__ __launch_bounds__(256) void linear_any(LinearArgs a) {
                 for (int j = 0; j < 4; ++j) acc[i][j] = mfma<E>(fw[i], fx[j], acc[i][j]);
         }
     }
-    epilogue<E, ACT>(a, acc, __builtin_amdgcn_readfirstlane(m0 + wm), __builtin_amdgcn_readfirstlane(n0 + wn));
+    if constexpr (ACT == kPart) store_part(a, acc, ((int64_t)blockIdx.x * 4 + wave) * 4);
+    else epilogue<E, ACT>(a, acc, __builtin_amdgcn_readfirstlane(m0 + wm), __builtin_amdgcn_readfirstlane(n0 + wn));
+}
+
+// Joins the parts of K, in their order, and finishes: a wave per 64 channels x 16 tokens of tiles of WN x WM waves of 64 channels x 16 FM tokens.
+template <typename E, int ACT>
+__global__ __launch_bounds__(256) void linear_join(LinearArgs a, int FM, int WN, int WM, int group_n) {
+    const int lane = threadIdx.x & 63, per_tile = FM * WN * WM;
+    const int n_tiles = (a.N + 64 * WN - 1) / (64 * WN), m_tiles = (a.M + 16 * FM * WM - 1) / (16 * FM * WM);
+    const int64_t g = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), stride = (int64_t)n_tiles * m_tiles * per_tile * 256;
+    const int tile = (int)(g / per_tile), in = (int)(g - (int64_t)tile * per_tile), wave = in / FM, j = in - wave * FM;
+    if (tile >= n_tiles * m_tiles) return;
+    int m0, n0;
+    tile_origin(tile, m_tiles, n_tiles, group_n, 16 * FM * WM, 64 * WN, m0, n0);
+    m0 += wave / WN * 16 * FM + 16 * j;
+    n0 += wave % WN * 64;
+    if (m0 >= a.M || n0 >= a.N) return;
+    v4f acc[4][1] = {};
+    const float4 *p = a.parts + g * 256 + lane;
+#pragma unroll 2
+    for (int s = 0; s < a.splits; ++s, p += stride)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i][0] += __builtin_bit_cast(v4f, p[i * 64]);
+    epilogue<E, ACT>(a, acc, m0, n0);
 }
 
 // ---- rows of whole 16-byte pieces: operands straight into LDS
@@ -192,62 +233,72 @@ template <typename E, int ACT, int FM, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, int group_n) {
     constexpr int W = WN * WM, BN = 64 * WN, BM = 16 * FM * WM, FH = FM < 4 ? FM : 4, NH = FM / FH, P = 2 * NH;
     constexpr int LW = BN / 8 / W, LX = BM / 8 / W;          // loads of a wave per slice, 8 rows each
-    constexpr int kStores = 2 * FM;                          // of a wave per whole tile
+    constexpr int kStores = ACT == kPart ? 4 * FM : 2 * FM;  // of a wave per whole tile
     constexpr uint32_t kUnitW = BN * 128, kUnitX = BM * 128;
     extern __shared__ uint4 lds[];                           // weights: 3 units, tokens: 2
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n_tiles = (a.N + BN - 1) / BN, m_tiles = (a.M + BM - 1) / BM, tiles = n_tiles * m_tiles, grid = gridDim.x;
+    const int n_tiles = (a.N + BN - 1) / BN, m_tiles = (a.M + BM - 1) / BM, tiles = n_tiles * m_tiles, items = tiles * a.splits, grid = gridDim.x;
     const int wn = wave % WN * 64, wm = wave / WN * 16 * FM;
-    const int slices = max(2, (a.K + 63) >> 6);
+    const int slices = a.slices;                             // at least 2; what lies past K is zero
 
     // Consecutive workgroups go to different XCDs.  Each XCD has one run of tiles, which its workgroups take in order: those that run
     // at the same time share panels, and so do those of the next round (as interleaved rounds of the whole chip, 32760 x 13824 x 5120
     // took 3340 us in place of 3190).
     const int xcds = min(8, grid), xcd = blockIdx.x % xcds, step = (grid - xcd + xcds - 1) / xcds;
-    const int end = (int)((int64_t)tiles * (xcd + 1) / xcds);
+    const int end = (int)((int64_t)items * (xcd + 1) / xcds);
     const uint32_t lds_w = lds_address(lds) + wave * (1024 * LW), lds_x = lds_address(lds) + 3 * kUnitW + wave * (1024 * LX);
     const uint8_t *src_w, *src_x;
     uint32_t off_w[LW], off_x[LX];
-    int m0, n0;
-    auto aim = [&](int t) {                                  // the loads' source: tile t
-        tile_origin(t, m_tiles, n_tiles, group_n, BM, BN, m0, n0);
-        src_w = reinterpret_cast<const uint8_t *>(uniform_ptr(a.w + n0 * a.ldw));
-        src_x = reinterpret_cast<const uint8_t *>(uniform_ptr(a.x + m0 * a.ldx));
+    const bool spread_w = a.N * a.ldw < (int64_t)1 << 31, spread_x = a.M * a.ldx < (int64_t)1 << 31;   // offsets of 32 bits
+    int m0, n0, k_left;
+    auto aim = [&](int t) {                                  // the loads' source: part t / tiles of K of tile t % tiles
+        const int part = ACT == kPart ? t / tiles : 0, k0 = part * slices * 64;
+        tile_origin(t - part * tiles, m_tiles, n_tiles, group_n, BM, BN, m0, n0);
+        k_left = a.K - k0;
+        // Rows past the matrix are read from other rows of it (their products are dropped), spread over it: the last row for all of them
+        // is one line that every workgroup of a column of tiles asks for at once (24017 x 3608 x 176, 256-channel tiles, 118 us).
+        const int base_n = spread_w && n0 + BN > a.N ? 0 : n0, base_m = spread_x && m0 + BM > a.M ? 0 : m0;
+        src_w = reinterpret_cast<const uint8_t *>(uniform_ptr(a.w + (base_n * a.ldw + k0)));
+        src_x = reinterpret_cast<const uint8_t *>(uniform_ptr(a.x + (base_m * a.ldx + k0)));
+        auto inside = [](int row, int first, int rows, int base) {
+            row += first;
+            return (row < rows ? row : base + (row - base) % (rows - base)) - base;
+        };
 #pragma unroll
         for (int j = 0; j < LW; ++j) {
             const int row = wave * (8 * LW) + 8 * j + (lane >> 3);
-            off_w[j] = (uint32_t)(min(channel_of_row(row), a.N - 1 - n0) * a.ldw * 2) + 16 * ((lane & 7) ^ ((row >> 1) & 7));
+            off_w[j] = (uint32_t)(inside(channel_of_row(row), n0, a.N, base_n) * a.ldw * 2) + 16 * ((lane & 7) ^ ((row >> 1) & 7));
         }
 #pragma unroll
         for (int j = 0; j < LX; ++j) {
             const int row = wave * (8 * LX) + 8 * j + (lane >> 3);
-            off_x[j] = (uint32_t)(min(row, a.M - 1 - m0) * a.ldx * 2) + 16 * ((lane & 7) ^ ((row >> 1) & 7));
+            off_x[j] = (uint32_t)(inside(row, m0, a.M, base_m) * a.ldx * 2) + 16 * ((lane & 7) ^ ((row >> 1) & 7));
         }
     };
     // slice q of the aimed tile; `whole`: known to lie within K
     auto load_w = [&](int q, int slot, bool whole) {
         const uint8_t *src = src_w + (uint32_t)q * 128u;
-        if (whole || (q + 1) * 64 <= a.K) {
+        if (whole || (q + 1) * 64 <= k_left) {
 #pragma unroll
             for (int j = 0; j < LW; ++j) lds_direct_load16(src, off_w[j], lds_w + slot * kUnitW + 1024 * j);
         } else {
 #pragma unroll
             for (int j = 0; j < LW; ++j) {
                 const int piece = 16 * ((lane & 7) ^ (((wave * (8 * LW) + 8 * j + (lane >> 3)) >> 1) & 7));
-                lds_direct_load16_at(piece < (a.K - q * 64) * 2 ? static_cast<const void *>(src + off_w[j]) : &zero_piece, lds_w + slot * kUnitW + 1024 * j);
+                lds_direct_load16_at(piece < (k_left - q * 64) * 2 ? static_cast<const void *>(src + off_w[j]) : &zero_piece, lds_w + slot * kUnitW + 1024 * j);
             }
         }
     };
     auto load_x = [&](int q, int slot, bool whole) {
         const uint8_t *src = src_x + (uint32_t)q * 128u;
-        if (whole || (q + 1) * 64 <= a.K) {
+        if (whole || (q + 1) * 64 <= k_left) {
 #pragma unroll
             for (int j = 0; j < LX; ++j) lds_direct_load16(src, off_x[j], lds_x + slot * kUnitX + 1024 * j);
         } else {
 #pragma unroll
             for (int j = 0; j < LX; ++j) {
                 const int piece = 16 * ((lane & 7) ^ (((wave * (8 * LX) + 8 * j + (lane >> 3)) >> 1) & 7));
-                lds_direct_load16_at(piece < (a.K - q * 64) * 2 ? static_cast<const void *>(src + off_x[j]) : &zero_piece, lds_x + slot * kUnitX + 1024 * j);
+                lds_direct_load16_at(piece < (k_left - q * 64) * 2 ? static_cast<const void *>(src + off_x[j]) : &zero_piece, lds_x + slot * kUnitX + 1024 * j);
             }
         }
     };
@@ -267,7 +318,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
         for (int f = 0; f < FH; ++f) fx[p & 1][f] = lds[sx * (kUnitX / 16) + (at_x ^ (4 * ks)) + 128 * (h * FH + f)];
     };
 
-    int t = (int)((int64_t)tiles * xcd / xcds) + blockIdx.x / xcds, sw = 0, sx = 0;   // places of the present slice
+    int t = (int)((int64_t)items * xcd / xcds) + blockIdx.x / xcds, sw = 0, sx = 0;   // places of the present slice
     if (t >= end) return;
     aim(t);
     load_w(0, 0, false);
@@ -279,7 +330,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
     read(0, 0, 0);
     bool stored = false;                                     // the outputs of a whole tile are on their way
     while (true) {
-        const int cur_m = m0, cur_n = n0, next = t + step;
+        const int cur_m = m0, cur_n = n0, next = t + step, whole = min(slices - 3, (k_left >> 6) - 2);
         // STEADY: slices of this tile follow, all within K
         auto slice = [&](int q, auto steady) {
             constexpr bool STEADY = decltype(steady)::value;
@@ -318,14 +369,15 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
 #pragma unroll 1
         for (int q = 0; q < slices; ++q) {
             if (q == steady)
-                for (; q < slices - 3; ++q) slice(q, std::true_type());
+                for (; q < whole; ++q) slice(q, std::true_type());
             slice(q, std::false_type());
         }
-        epilogue<E, ACT>(a, acc, cur_m + wm, cur_n + wn);
+        if constexpr (ACT == kPart) store_part(a, acc, ((int64_t)t * W + wave) * FM);
+        else epilogue<E, ACT>(a, acc, cur_m + wm, cur_n + wn);
         if (next >= end) return;
         read(sw, sx, 0);
         t = next;
-        stored = cur_m + BM <= a.M && cur_n + BN <= a.N;
+        stored = ACT == kPart || (cur_m + BM <= a.M && cur_n + BN <= a.N);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -334,30 +386,91 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
 }
 
 template <typename E, int ACT, int FM, int WN, int WM>
-int launch_tiles(const LinearArgs &a, int per_cu, hipStream_t stream) {
+int launch_tiles(const LinearArgs &a, int per_cu, int group_n, hipStream_t stream) {
     constexpr int BN = 64 * WN, BM = 16 * FM * WM;
     constexpr size_t kLds = (3 * BN + 2 * BM) * 128;
     static std::atomic<uint64_t> done{0};
     const auto kernel = linear_tiles<E, ACT, FM, WN, WM>;
     allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kLds, done);
-    const int n_tiles = (a.N + BN - 1) / BN, tiles = n_tiles * ((a.M + BM - 1) / BM);
-    // columns of tiles that are run through before the next row: panels of either side are shared by the workgroups of an XCD
-    const int groups = (n_tiles + 5) / 6;
-    kernel<<<dim3(min(tiles, 256 * per_cu)), 64 * WN * WM, kLds, stream>>>(a, (n_tiles + groups - 1) / groups);
+    const int items = ((a.N + BN - 1) / BN) * ((a.M + BM - 1) / BM) * a.splits;
+    kernel<<<dim3(min(items, 256 * per_cu)), 64 * WN * WM, kLds, stream>>>(a, group_n);
     return check_launch();
+}
+
+// The shapes of tiles: channels, tokens, workgroups per compute unit (LDS)
+struct Shape { int fm, wn, wm, per_cu; };
+constexpr Shape kShapes[] = {{8, 4, 2, 1}, {4, 4, 2, 1}, {4, 2, 2, 2}, {2, 2, 2, 2}, {2, 1, 2, 4}};
+constexpr int kShapeAny = 2;   // linear_any's
+
+struct LinearPlan { int shape, splits, slices, group_n; size_t parts_bytes; };
+
+// Estimated time of a shape of tile and a number of parts of K, in us.  A slice takes a workgroup 0.27 us and 0.75 us per 64 KB of it, or, where
+// its compute unit is busy, its share of the loads (162 GB/s for one compute unit alone, 74 where all of them load) and of the matrix
+// cores (1.44 us for 256 x 256 x 64).  A round of tiles has 0.6 us and 4.7 us per 256 x 256 of outputs beside its slices, 6.3 where one workgroup
+// has the compute unit for itself and nothing hides its outputs.  Parts of K are written and read back at 11.5 TB/s (they stay in the caches),
+// by a launch of 2.6 us.  The constants are fitted to some 1000 timings of 68 outputs (32 to 118800 tokens, 64 to 11384 channels, K 64 to 13824)
+// with every shape and 1 to 12 parts: the choice takes 5 % longer than the best of them in the mean, 52 % at most; always 128 x 128 without parts
+// 50 % in the mean, 7.6 times at most.
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
+    const int total = (int)((K + 63) / 64);
+    LinearPlan best = {};
+    float best_time = 1e30f;
+    for (int i = 0; i < (int)(sizeof(kShapes) / sizeof(kShapes[0])); ++i) {
+        if (any && i != kShapeAny) continue;
+        const Shape &sh = kShapes[i];
+        const int bn = 64 * sh.wn, bm = 16 * sh.fm * sh.wm, n_tiles = (int)((N + bn - 1) / bn), slots = 256 * sh.per_cu;
+        const int64_t tiles = n_tiles * ((M + bm - 1) / bm);
+        const float area = (float)(bn * bm) / 65536, bytes = (float)((bn + bm) * 128);
+        for (const int want : {1, 2, 3, 4, 6, 8, 12}) {
+            const int per = std::max(2, (total + want - 1) / want), splits = (total + per - 1) / per;
+            if (want > 1 && (per < 4 || splits == 1 || tiles * splits > slots)) break;
+            const int64_t items = tiles * splits, full = items / slots;
+            const int rest = (int)(items - full * slots);
+            const float load = bytes * (1 / 162e3f + (items < 256 ? (float)items / 256 : 1.0f) / 138e3f), lone = 0.27f + 0.75f / 65536 * bytes;
+            auto round = [&](int resident) {
+                return 0.6f + (4.7f * (float)resident + (sh.per_cu == 1 ? 1.6f : 0.0f)) * area +
+                       (float)per * std::max(lone, (float)resident * std::max(load, 1.44f * area));
+            };
+            float time = (float)full * round(sh.per_cu) + (rest ? round((rest + 255) / 256) : 0.0f);
+            if (splits > 1) time += 2.6f + (float)items * area * (8 * 65536 / 11.5e6f);
+            if (time < best_time) {
+                best_time = time;
+                const int groups = (n_tiles + 5) / 6;   // columns of tiles that are run through before the next row
+                best = {i, splits, per, any ? n_tiles : (n_tiles + groups - 1) / groups, splits > 1 ? (size_t)(items * bn * bm) * sizeof(float) : 0};
+            }
+        }
+    }
+    return best;
+}
+
+template <typename E, int ACT>
+int launch_product(const LinearArgs &a, const LinearPlan &p, bool any, hipStream_t stream) {
+    if (any) {
+        static std::atomic<uint64_t> done{0};
+        constexpr size_t kLds = 2 * 256 * 128;
+        allow_dynamic_lds(reinterpret_cast<const void *>(linear_any<E, ACT>), kLds, done);
+        linear_any<E, ACT><<<dim3((unsigned)(((a.N + 127) / 128) * ((a.M + 127) / 128) * a.splits)), 256, kLds, stream>>>(a);
+        return check_launch();
+    }
+    switch (p.shape) {
+        case 0: return launch_tiles<E, ACT, 8, 4, 2>(a, 1, p.group_n, stream);
+        case 1: return launch_tiles<E, ACT, 4, 4, 2>(a, 1, p.group_n, stream);
+        case 2: return launch_tiles<E, ACT, 4, 2, 2>(a, 2, p.group_n, stream);
+        case 3: return launch_tiles<E, ACT, 2, 2, 2>(a, 2, p.group_n, stream);
+        default: return launch_tiles<E, ACT, 2, 1, 2>(a, 4, p.group_n, stream);
+    }
 }
 
 }  // namespace
 
 size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    (void)M, (void)N, (void)K;
-    return 0;
+    const size_t any = linear_plan(M, N, K, true).parts_bytes;   // (addresses and pitches are not known here)
+    return K % 8 == 0 ? std::max(any, linear_plan(M, N, K, false).parts_bytes) : any;
 }
 
 int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias, int act, const void *gate, int64_t gate_rows,
                   int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype, void *y, int64_t ldy,
                   void *workspace, hipStream_t stream) {
-    (void)workspace;
     LinearArgs a = {};
     a.x = static_cast<const uint16_t *>(x), a.w = static_cast<const uint16_t *>(w), a.bias = static_cast<const uint16_t *>(bias);
     a.gate = static_cast<const uint16_t *>(gate), a.residual = static_cast<const uint16_t *>(residual), a.y = static_cast<uint16_t *>(y);
@@ -365,17 +478,22 @@ int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const 
     a.M = (int)M, a.N = (int)N, a.K = (int)K;
     a.gate_rows = gate ? (int)(M / gate_rows) : 1;
     const auto whole = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 7) == 0 && ld < (int64_t)1 << 22; };
-    const bool pieces = K % 8 == 0 && whole(x, M > 1 ? ldx : 0) && whole(w, N > 1 ? ldw : 0);
+    const bool any = K % 8 != 0 || !whole(x, M > 1 ? ldx : 0) || !whole(w, N > 1 ? ldw : 0);
+    const LinearPlan p = linear_plan(M, N, K, any);
+    a.parts = static_cast<float4 *>(workspace);
+    a.splits = p.splits;
+    a.slices = p.slices;
     return with_type(dtype, [&](auto type) {
         using E = decltype(type);
         if constexpr (sizeof(typename E::Raw) == 2) {
             return with_act(act, [&](auto which) {
                 constexpr int ACT = decltype(which)::value;
-                if (pieces) {
-                    if (((M + 255) / 256) * ((N + 255) / 256) >= 256) return launch_tiles<E, ACT, 8, 4, 2>(a, 1, stream);
-                    return launch_tiles<E, ACT, 4, 2, 2>(a, 2, stream);
-                }
-                linear_any<E, ACT><<<dim3((unsigned)(((N + 127) / 128) * ((M + 127) / 128))), 256, 0, stream>>>(a);
+                if (p.splits == 1) return launch_product<E, ACT>(a, p, any, stream);
+                const int rc = launch_product<E, kPart>(a, p, any, stream);
+                if (rc != DVDQ_OK) return rc;
+                const Shape &sh = kShapes[p.shape];
+                const int64_t waves = ((N + 64 * sh.wn - 1) / (64 * sh.wn)) * ((M + 16 * sh.fm * sh.wm - 1) / (16 * sh.fm * sh.wm)) * sh.fm * sh.wn * sh.wm;
+                linear_join<E, ACT><<<dim3((unsigned)((waves + 3) / 4)), 256, 0, stream>>>(a, sh.fm, sh.wn, sh.wm, p.group_n);
                 return check_launch();
             });
         } else {
