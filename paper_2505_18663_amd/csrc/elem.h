@@ -42,10 +42,17 @@ static __device__ __forceinline__ Piece<E, V> load_piece(const typename E::Raw *
         if (i < n) r.e[i] = p[i];
     return r;
 }
-template <typename E, int V = E::kVec>
+// STREAM: past the caches, for outputs that are larger than those and whose pieces make whole lines between them
+template <typename E, int V = E::kVec, bool STREAM = false>
 static __device__ __forceinline__ void store_piece(typename E::Raw *p, const Piece<E, V> &v, int n) {
     if (n >= V) {
-        *reinterpret_cast<Piece<E, V> *>(p) = v;
+        if constexpr (STREAM && sizeof(v) == 16) {
+            typedef uint32_t Quad __attribute__((ext_vector_type(4)));
+            typedef Quad Anywhere __attribute__((aligned(2)));
+            __builtin_nontemporal_store(__builtin_bit_cast(Quad, v), reinterpret_cast<Anywhere *>(p));
+        } else {
+            *reinterpret_cast<Piece<E, V> *>(p) = v;
+        }
         return;
     }
 #pragma unroll

@@ -5,6 +5,8 @@
 // mean and var (biased) over the S rows and the C / groups channels of a group.  Every few rows of a channel are summed up, then their
 // squared deviations from their own mean, and parts are joined by count, mean and sum of squared deviations: channels far from zero
 // and rows unlike the others lose nothing (differences to a value picked beforehand do, where that value is such a row's).
+#include <algorithm>
+
 #include "elem.h"
 #include "wave_reduce.h"
 
@@ -124,32 +126,111 @@ __global__ __launch_bounds__(1024) void gn_parts(GnArgs a) {
     }
 }
 
-// A wave joins the parts of one group of one batch.
-__global__ __launch_bounds__(64) void gn_join(GnArgs a) {
+// The sum over a workgroup, the same in every thread.  `lds`: a word per wave, free on entry; free again behind the next barrier.
+template <typename T>
+static __device__ __forceinline__ T block_sum(T v, T *lds) {
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    T sum = lds[0];
+    for (int i = 1; i < (int)(blockDim.x >> 6); ++i) sum += lds[i];
+    return sum;
+}
+
+// A workgroup joins the parts of one group of one batch, all of them in registers (kMaxSlabs).
+constexpr int kMaxSlabs = 2048, kPerThread = kMaxSlabs / 256;
+__global__ __launch_bounds__(256) void gn_join(GnArgs a) {
+    __shared__ double lds[2][4];
     const int g = blockIdx.x, b = blockIdx.y;
     const Moments *p = a.parts + (int64_t)b * a.slabs * a.groups + g;
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < a.slabs; i += 64) {
-        const int64_t rows = min(a.S - i * a.slab_rows, a.slab_rows);
-        sum += (double)rows * p[(int64_t)i * a.groups].mean;
+    Moments m[kPerThread];
+    double rows[kPerThread], sum = 0.0, m2 = 0.0;
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+        const int slab = threadIdx.x + 256 * i;
+        if (slab < a.slabs) m[i] = p[(int64_t)slab * a.groups];
+        else m[i] = {};
+        rows[i] = slab < a.slabs ? (double)min(a.S - slab * a.slab_rows, a.slab_rows) : 0.0;
     }
-    const double mean = wave_sum(sum) / (double)a.S;
-    double m2 = 0.0;
-    for (int i = threadIdx.x; i < a.slabs; i += 64) {
-        const int64_t rows = min(a.S - i * a.slab_rows, a.slab_rows);
-        const Moments m = p[(int64_t)i * a.groups];
-        const double d = (double)m.mean - mean;
-        m2 += m.m2 + (double)(rows * a.cpg) * d * d;
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i)
+        if (rows[i] > 0.0) sum += rows[i] * m[i].mean;
+    const double mean = block_sum(sum, lds[0]) / (double)a.S;
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+        const double d = (double)m[i].mean - mean;
+        if (rows[i] > 0.0) m2 += m[i].m2 + rows[i] * a.cpg * d * d;
     }
-    const double var = wave_sum(m2) / ((double)a.S * a.cpg);
+    const double var = block_sum(m2, lds[1]) / ((double)a.S * a.cpg);
     if (threadIdx.x == 0) a.stats[b * a.groups + g] = make_float2((float)mean, (float)(1.0 / sqrt(var + (double)a.eps)));
 }
 
-template <typename E, int ACT>
+// A whole group in a workgroup's registers: read once, written once, one launch.  V: elements of a piece of a row of the group.
+constexpr int kUnits = 8;
+template <typename E, int ACT, int V>
+__global__ __launch_bounds__(1024) void gn_whole(GnArgs a) {
+    using Raw = typename E::Raw;
+    __shared__ float lds[2][16];
+    const int g = blockIdx.x, b = blockIdx.y, threads = blockDim.x;
+    const int per_row = a.cpg / V, total = (int)a.S * per_row;
+    const Raw *x = static_cast<const Raw *>(a.x) + b * a.x_batch + g * a.cpg;
+    Raw *y = static_cast<Raw *>(a.y) + b * a.y_batch + g * a.cpg;
+    const int row0 = threadIdx.x / per_row, c0 = threadIdx.x - row0 * per_row, d_row = threads / per_row, d_c = threads - d_row * per_row;
+    Piece<E, V> p[kUnits];
+    {
+        int row = row0, c = c0;
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            if ((int)threadIdx.x + i * threads < total) p[i] = load_piece<E, V>(x + row * a.x_row + c * V, V);
+            else p[i] = Piece<E, V>{};
+            row += d_row, c += d_c;
+            if (c >= per_row) c -= per_row, ++row;
+        }
+    }
+    const float first = E::to_f32(x[0]), count = (float)((int)a.S * a.cpg);
+    float sum = 0.0f, m2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+        if ((int)threadIdx.x + i * threads < total) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum += E::to_f32(p[i].e[j]) - first;
+        }
+    const float mean = first + block_sum(sum, lds[0]) / count;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i)
+        if ((int)threadIdx.x + i * threads < total) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float d = E::to_f32(p[i].e[j]) - mean;
+                m2 = fmaf(d, d, m2);
+            }
+        }
+    const float rstd = (float)(1.0 / sqrt((double)block_sum(m2, lds[1]) / (double)count + (double)a.eps));
+    int row = row0, c = c0;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) {
+        if ((int)threadIdx.x + i * threads < total) {
+            const int ch = g * a.cpg + c * V;
+            Piece<E, V> w, bias;
+            if (a.weight) w = load_piece<E, V>(static_cast<const Raw *>(a.weight) + ch, V);
+            if (a.bias) bias = load_piece<E, V>(static_cast<const Raw *>(a.bias) + ch, V);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float scale = a.weight ? rstd * E::to_f32(w.e[j]) : rstd, shift = a.bias ? E::to_f32(bias.e[j]) : 0.0f;
+                p[i].e[j] = E::from_f32(activate<ACT>(fmaf(E::to_f32(p[i].e[j]) - mean, scale, shift)));
+            }
+            store_piece<E, V>(y + row * a.y_row + c * V, p[i], V);
+        }
+        row += d_row, c += d_c;
+        if (c >= per_row) c -= per_row, ++row;
+    }
+}
+
+template <typename E, int ACT, bool STREAM>
 __global__ __launch_bounds__(1024) void gn_apply(GnArgs a) {
     using Raw = typename E::Raw;
-    constexpr int V = E::kVec;
-    const int b = blockIdx.y;
+    constexpr int V = E::kVec, kRows = 4;                // rows of a thread that are on their way at a time
+    const int b = gridDim.y - 1 - blockIdx.y, slab = gridDim.x - 1 - blockIdx.x;   // backwards: what was read last is still in the caches
     const int r = threadIdx.x / a.cols, col = threadIdx.x - r * a.cols, c0 = col * V, n = min(V, a.C - c0);
     if (r >= a.rows_at_once) return;
     float mean[V], scale[V], shift[V];
@@ -161,14 +242,23 @@ __global__ __launch_bounds__(1024) void gn_apply(GnArgs a) {
         scale[i] = st.y * (a.weight ? E::to_f32(static_cast<const Raw *>(a.weight)[c]) : 1.0f);
         shift[i] = a.bias ? E::to_f32(static_cast<const Raw *>(a.bias)[c]) : 0.0f;
     }
-    const Raw *x = static_cast<const Raw *>(a.x) + b * a.x_batch + c0;
-    Raw *y = static_cast<Raw *>(a.y) + b * a.y_batch + c0;
-    const int64_t s0 = blockIdx.x * a.slab_rows, s1 = min(a.S, s0 + a.slab_rows);
-    for (int64_t s = s0 + r; s < s1; s += a.rows_at_once) {
-        Piece<E> p = load_piece<E>(x + s * a.x_row, n);
+    const int64_t s0 = slab * a.slab_rows;
+    const int rows = (int)min(a.S - s0, a.slab_rows), mine = (rows - r + a.rows_at_once - 1) / a.rows_at_once;
+    const int64_t x_step = a.rows_at_once * a.x_row, y_step = a.rows_at_once * a.y_row;
+    const Raw *x = static_cast<const Raw *>(a.x) + (b * a.x_batch + (s0 + r) * a.x_row + c0);
+    Raw *y = static_cast<Raw *>(a.y) + (b * a.y_batch + (s0 + r) * a.y_row + c0);
+    for (int i0 = 0; i0 < mine; i0 += kRows, x += kRows * x_step, y += kRows * y_step) {
+        Piece<E> p[kRows];
 #pragma unroll
-        for (int i = 0; i < V; ++i) p.e[i] = E::from_f32(activate<ACT>(fmaf(E::to_f32(p.e[i]) - mean[i], scale[i], shift[i])));
-        store_piece<E>(y + s * a.y_row, p, n);
+        for (int i = 0; i < kRows; ++i)
+            if (i0 + i < mine) p[i] = load_piece<E>(x + i * x_step, n);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            if (i0 + i >= mine) break;
+#pragma unroll
+            for (int j = 0; j < V; ++j) p[i].e[j] = E::from_f32(activate<ACT>(fmaf(E::to_f32(p[i].e[j]) - mean[j], scale[j], shift[j])));
+            store_piece<E, V, STREAM>(y + i * y_step, p[i], n);
+        }
     }
 }
 
@@ -182,7 +272,7 @@ Plan plan(int64_t B, int64_t S, int64_t C, int64_t groups, int vec) {
     const int64_t want = max((int64_t)1, (int64_t)2048 / B);                              // workgroups to fill the chip
     p.slab_rows = max((S + want - 1) / want, (int64_t)8 * p.rows_at_once);
     p.slab_rows = (p.slab_rows + p.rows_at_once - 1) / p.rows_at_once * p.rows_at_once;
-    p.slabs = (int)((S + p.slab_rows - 1) / p.slab_rows);
+    p.slabs = (int)((S + p.slab_rows - 1) / p.slab_rows);   // at most kMaxSlabs
     p.parts_bytes = ((size_t)B * p.slabs * groups * sizeof(Moments) + 255) / 256 * 256;
     p.stats_bytes = ((size_t)B * groups * sizeof(float2) + 255) / 256 * 256;
     return p;
@@ -213,11 +303,26 @@ int launch_group_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_
         a.eps = eps;
         a.parts = static_cast<Moments *>(workspace);
         a.stats = reinterpret_cast<float2 *>(static_cast<uint8_t *>(workspace) + p.parts_bytes);
+        const bool silu = act == DVDQ_ACT_SILU;
+        const auto one_launch = [&](auto width) {
+            constexpr int V = decltype(width)::value;
+            const int64_t total = S * (a.cpg / V);
+            if (a.cpg % V != 0 || total > 1024 * kUnits) return false;
+            const int threads = (int)std::clamp((total + 127) / 128 * 64, (int64_t)64, (int64_t)1024);   // two pieces a thread, up to 16 waves
+            const auto kernel = silu ? gn_whole<E, DVDQ_ACT_SILU, V> : gn_whole<E, DVDQ_ACT_NONE, V>;
+            kernel<<<dim3((unsigned)groups, (unsigned)B), threads, 0, stream>>>(a);
+            return true;
+        };
+        if (one_launch(std::integral_constant<int, E::kVec>()) || (E::kVec > 4 && one_launch(std::integral_constant<int, 4>())) ||
+            one_launch(std::integral_constant<int, 2>()) || one_launch(std::integral_constant<int, 1>()))
+            return check_launch();
         const dim3 grid(p.slabs, (unsigned)B);
         gn_parts<E><<<grid, p.threads, (size_t)p.rows_at_once * 2 * p.cols * E::kVec * sizeof(float), stream>>>(a);
-        gn_join<<<dim3((unsigned)groups, (unsigned)B), 64, 0, stream>>>(a);
-        if (act == DVDQ_ACT_SILU) gn_apply<E, DVDQ_ACT_SILU><<<grid, p.threads, 0, stream>>>(a);
-        else gn_apply<E, DVDQ_ACT_NONE><<<grid, p.threads, 0, stream>>>(a);
+        gn_join<<<dim3((unsigned)groups, (unsigned)B), 256, 0, stream>>>(a);
+        const bool stream_out = (int64_t)B * S * C * (int64_t)sizeof(typename E::Raw) >= (4 << 20);
+        const auto apply = silu ? (stream_out ? gn_apply<E, DVDQ_ACT_SILU, true> : gn_apply<E, DVDQ_ACT_SILU, false>)
+                                : (stream_out ? gn_apply<E, DVDQ_ACT_NONE, true> : gn_apply<E, DVDQ_ACT_NONE, false>);
+        apply<<<grid, p.threads, 0, stream>>>(a);
         return check_launch();
     });
 }

@@ -4,6 +4,8 @@
 //
 // for every pair j of a head: elements 2j and 2j+1 (interleaved) or j and j + R/2 (halves) of the first R elements; the rest of the
 // head is copied.  Products and sums in fp32, one rounding to the tensors' type.
+#include <algorithm>
+
 #include "elem.h"
 
 namespace dvdq {
@@ -11,7 +13,7 @@ namespace dvdq {
 namespace {
 
 constexpr int kMaxAxes = 4;
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kHeadsPerThread = 6;
 
 struct RopeKernelArgs {
     const void *in[2];
@@ -33,11 +35,14 @@ struct RopeKernelArgs {
 
 // A thread owns one piece of the head (16 bytes of each half of the pairs, or 16 bytes of interleaved pairs) for one token, and
 // goes through heads: the token's cosines and sines are read once and stay in registers.  Neighbouring threads hold neighbouring
-// pieces, so a wave reads and writes whole heads.
-template <typename E, bool INTERLEAVED>
+// pieces, so a wave reads and writes whole heads.  Up to six heads of a thread are in flight at a time.
+// Bound by memory: 118800 tokens x 48 heads of 128 in 16 bits, 2.9 GB in and out, in 490 us (6.0 TB/s; a copy on the same card 5.9),
+// 32760 x 24 in 70 (5.8).  What it took: cosines and sines in 16-byte loads where a piece lies within one axis (780 -> 637 us, one by
+// one), streaming stores (-> 532), six heads a thread (-> 490).
+template <typename E, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeKernelArgs a) {
     using Raw = typename E::Raw;
-    constexpr int V = E::kVec, PAIRS = INTERLEAVED ? V / 2 : V, BATCH = 4;
+    constexpr int V = E::kVec, PAIRS = INTERLEAVED ? V / 2 : V, BATCH = kHeadsPerThread;
     const int per_token = a.units * a.heads_at_once;
     const int lt = (int)threadIdx.x / per_token, rem = (int)threadIdx.x - lt * per_token;
     const uint32_t token = blockIdx.x * (uint32_t)a.tokens_per_block + lt;
@@ -61,6 +66,17 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeKernelArgs a) {
         int p[kMaxAxes];
 #pragma unroll
         for (int i = 0; i < kMaxAxes; ++i) p[i] = i < a.n_axes ? pos[i] : 0;
+        const auto axis_of = [&](int j) { return j < a.bound[0] ? 0 : j < a.bound[1] ? 1 : j < a.bound[2] ? 2 : 3; };
+        const int axis = axis_of(j0), one = axis == 0 ? p[0] : axis == 1 ? p[1] : axis == 2 ? p[2] : p[3];
+        if (np == PAIRS && axis == axis_of(j0 + PAIRS - 1) && one >= 0 && one < a.n_pos) {
+            struct __attribute__((packed, aligned(8))) Row { float2 v[PAIRS]; };
+            const Row row = *reinterpret_cast<const Row *>(a.table + (int64_t)one * half + j0);
+#pragma unroll
+            for (int i = 0; i < PAIRS; ++i) {
+                c[i] = row.v[i].x;
+                s[i] = a.inverse ? -row.v[i].y : row.v[i].y;
+            }
+        } else
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) {
             const int j = j0 + i;
@@ -102,13 +118,13 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeKernelArgs a) {
                     Raw &rb = INTERLEAVED ? lo[i].e[2 * k + 1] : hi[i].e[k];
                     const float x = E::to_f32(ra), y = E::to_f32(rb);
                     if (!(keep >> k & 1)) {
-                        ra = E::from_f32(x * c[k] - y * s[k]);
-                        rb = E::from_f32(x * s[k] + y * c[k]);
+                        ra = E::from_f32(fmaf(x, c[k], -(y * s[k])));
+                        rb = E::from_f32(fmaf(x, s[k], y * c[k]));
                     }
                 }
             }
-            store_piece<E>(dst[i], lo[i], n);
-            if (!INTERLEAVED && rotated) store_piece<E>(dst[i] + half, hi[i], n);
+            store_piece<E, V, STREAM>(dst[i], lo[i], n);
+            if (!INTERLEAVED && rotated) store_piece<E, V, STREAM>(dst[i] + half, hi[i], n);
         }
     }
 }
@@ -167,12 +183,22 @@ int launch_rope(const dvdq_rope_heads *q, const dvdq_rope_heads *k, int64_t B, i
         a.rot_units = (int)((R + per_unit - 1) / per_unit);
         // (in place, the part that is not rotated stays where it is)
         a.units = a.rot_units + (in_place ? 0 : (int)((D - R + E::kVec - 1) / E::kVec));
-        a.heads_at_once = min(a.heads, max(1, 64 / a.units));
-        a.tokens_per_block = max(1, kThreads / (a.units * a.heads_at_once));
-        a.heads_per_block = a.heads;
+        // heads of a thread: as many as are in flight at a time, fewer where that leaves the chip with less than 512 threads per compute unit
+        // (and, where a head is no whole lines, so that those that a token's threads write at once are 384 bytes at least: 46400 x 6 heads
+        // of 72 16.5 us with three at once, 24 with one)
+        const int head_bytes = (int)(D * sizeof(typename E::Raw)), at_once = head_bytes % 128 == 0 ? 1 : (383 + head_bytes) / head_bytes;
+        int per_thread = std::clamp(a.heads / at_once, 1, kHeadsPerThread);
+        while (per_thread > 1 && (int64_t)a.tokens * a.units * ((a.heads + per_thread - 1) / per_thread) < 256 * 512) --per_thread;
+        a.heads_at_once = std::min((a.heads + per_thread - 1) / per_thread, std::max(1, kThreads / a.units));
+        a.tokens_per_block = std::max(1, kThreads / (a.units * a.heads_at_once));
+        a.heads_per_block = a.heads_at_once * per_thread;
         const dim3 grid((a.tokens + a.tokens_per_block - 1) / a.tokens_per_block, (a.heads + a.heads_per_block - 1) / a.heads_per_block);
-        if (interleaved) rope_kernel<E, true><<<grid, kThreads, 0, stream>>>(a);
-        else rope_kernel<E, false><<<grid, kThreads, 0, stream>>>(a);
+        // Streaming stores from 4 MB on, which is what an XCD's L2 holds: 2000 x 40 heads of 128 9.4 us, cached 13.6; below that the
+        // outputs stay in the L2 for what reads them next (1022 x 16 heads of 80, 2.6 MB: 7.1 us, streaming 7.2).
+        const bool stream_out = (int64_t)a.tokens * a.heads * D * (int64_t)sizeof(typename E::Raw) >= (4 << 20);
+        const auto kernel = interleaved ? (stream_out ? rope_kernel<E, true, true> : rope_kernel<E, true, false>)
+                                        : (stream_out ? rope_kernel<E, false, true> : rope_kernel<E, false, false>);
+        kernel<<<grid, kThreads, 0, stream>>>(a);
         return check_launch();
     });
 }
