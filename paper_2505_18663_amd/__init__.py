@@ -70,7 +70,7 @@ class _Handback:
     @staticmethod
     def _hand_back(*args):
         return None
-    rotate_quant = rotate_quant_blockwise = w4ax_gemm = qlinear = gbs_reset = gbs_step = _hand_back
+    rotate_quant = rotate_quant_blockwise = w4ax_gemm = qlinear = gbs_reset = gbs_step = rope = linear = group_norm = _hand_back
 
 
 def _load_marshal(L):
@@ -83,7 +83,8 @@ def _load_marshal(L):
     spec.loader.exec_module(native)
     native.bind(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, *(C.cast(getattr(L, f), C.c_void_p).value for f in (
         "dvdq_rotate_quant", "dvdq_rotate_quant_blockwise", "dvdq_w4ax_gemm", "dvdq_qlinear", "dvdq_gbs_reset", "dvdq_gbs_step",
-        "dvdq_codes_bytes", "dvdq_qlinear_workspace_bytes", "dvdq_w4_native_bytes", "dvdq_w4_native_fp6_bytes")))
+        "dvdq_codes_bytes", "dvdq_qlinear_workspace_bytes", "dvdq_w4_native_bytes", "dvdq_w4_native_fp6_bytes",
+        "dvdq_rope", "dvdq_linear", "dvdq_linear_workspace_bytes", "dvdq_group_norm", "dvdq_group_norm_workspace_bytes")))
     return native
 
 
@@ -638,6 +639,9 @@ def rope(q, k, table, positions, sections=None, interleaved: bool = False, inver
     are.  q_out, k_out: where to, e.g. q and k themselves; new dense tensors otherwise.  inverse: the opposite angle, which is the
     backward pass.  Returns (q_out, k_out), or q_out alone without k.  See dvdq_rope."""
     L = lib()
+    r = _marshal.rope(q, k, table, positions, sections, interleaved, inverse, q_out, k_out, stream)
+    if r is not None:
+        return _native(r, "dvdq_rope")
     _need_view(q, None, None, "q")
     if q.dtype not in _DTYPES:
         raise TypeError(f"q: expected bfloat16, float16 or float32, got {q.dtype}")
@@ -678,6 +682,9 @@ def linear(x, w, bias=None, act: int = ACT_NONE, gate=None, residual=None, y=Non
     [N, K], both with rows of any pitch; bias [N]; gate [N] or [G, N], a row for each M / G consecutive tokens; residual [M, N], which
     y may be.  Returns y [M, N].  See dvdq_linear."""
     L = lib()
+    r = _marshal.linear(x, w, bias, act, gate, residual, y, workspace, stream)
+    if r is not None:
+        return _native(r, "dvdq_linear")
     _need_view(x, None, None, "x")
     if x.dtype not in (torch.bfloat16, torch.float16):
         raise TypeError(f"x: expected bfloat16 or float16, got {x.dtype}")
@@ -732,6 +739,9 @@ def group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, act: i
     x.movedim(1, -1)), statistics over the dimensions in between and each of `groups` runs of channels; weight and bias [C] of the same
     type; act ACT_NONE or ACT_SILU; y may be x.  Returns y.  See dvdq_group_norm."""
     L = lib()
+    r = _marshal.group_norm(x, groups, weight, bias, eps, act, y, workspace, stream)
+    if r is not None:
+        return _native(r, "dvdq_group_norm")
     _need_view(x, None, None, "x")
     if x.dtype not in _DTYPES:
         raise TypeError(f"x: expected bfloat16, float16 or float32, got {x.dtype}")

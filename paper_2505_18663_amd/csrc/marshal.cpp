@@ -29,6 +29,11 @@ decltype(&dvdq_codes_bytes) p_codes_bytes;
 decltype(&dvdq_qlinear_workspace_bytes) p_qlinear_workspace_bytes;
 decltype(&dvdq_w4_native_bytes) p_w4_native_bytes;
 decltype(&dvdq_w4_native_fp6_bytes) p_w4_native_fp6_bytes;
+decltype(&dvdq_rope) p_rope;
+decltype(&dvdq_linear) p_linear;
+decltype(&dvdq_linear_workspace_bytes) p_linear_workspace_bytes;
+decltype(&dvdq_group_norm) p_group_norm;
+decltype(&dvdq_group_norm_workspace_bytes) p_group_norm_workspace_bytes;
 
 PyObject *get_device, *get_raw_stream;   // torch._C's: number of the current device; its current stream's handle
 
@@ -47,16 +52,56 @@ struct Args {
         if (!ok || (optional && none(i))) return nullptr;
         if (THPVariable_CheckExact(a[i])) {
             const at::Tensor &t = THPVariable_Unpack(a[i]);
-            static const c10::DispatchKeySet wrapped({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchBatched,
-                                                      c10::DispatchKey::FuncTorchGradWrapper, c10::DispatchKey::Functionalize,
-                                                      c10::DispatchKey::Conjugate, c10::DispatchKey::Negative,
-                                                      c10::DispatchKey::ZeroTensor});
-            if (t.is_cuda() && t.scalar_type() == type && t.layout() == at::kStrided && t.is_contiguous() &&
-                !t.key_set().has_any(wrapped) && t.has_storage())
+            if (plain(t) && t.scalar_type() == type && t.is_contiguous()) return &t;
+        }
+        ok = false;
+        return nullptr;
+    }
+    static bool plain(const at::Tensor &t) {
+        static const c10::DispatchKeySet wrapped({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchBatched,
+                                                  c10::DispatchKey::FuncTorchGradWrapper, c10::DispatchKey::Functionalize,
+                                                  c10::DispatchKey::Conjugate, c10::DispatchKey::Negative, c10::DispatchKey::ZeroTensor});
+        return t.is_cuda() && t.layout() == at::kStrided && !t.key_set().has_any(wrapped) && t.has_storage();
+    }
+    // a view of `dim` dimensions with any strides whose last dimension is dense, of the type and on the device of `like` where one
+    // is given; None as with tensor()
+    const at::Tensor *view(int i, int64_t dim, const at::Tensor *like, bool optional = false) {
+        if (!ok || (optional && none(i))) return nullptr;
+        if (THPVariable_CheckExact(a[i])) {
+            const at::Tensor &t = THPVariable_Unpack(a[i]);
+            if (plain(t) && t.dim() == dim && t.numel() > 0 && (t.size(dim - 1) == 1 || t.stride(dim - 1) == 1) &&
+                (!like || (t.scalar_type() == like->scalar_type() && t.device() == like->device())))
                 return &t;
         }
         ok = false;
         return nullptr;
+    }
+    // the given view of that shape, or a new dense tensor of the type and on the device of `like`
+    at::Tensor output_like(int i, at::IntArrayRef shape, const at::Tensor &like) {
+        if (none(i)) return at::empty(shape, like.options());
+        const at::Tensor *t = view(i, (int64_t)shape.size(), &like);
+        if (!t || t->sizes() != shape) {
+            ok = false;
+            return at::Tensor();
+        }
+        return *t;
+    }
+    // scratch: the given bytes, or as many as are needed on the device of `like`
+    at::Tensor scratch(int i, size_t need, const at::Tensor &like) {
+        if (!none(i)) {
+            const at::Tensor *t = tensor(i, at::kByte);
+            return t ? *t : at::Tensor();
+        }
+        return need ? at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(like.device())) : at::Tensor();
+    }
+    // the library's number of a tensor's type (-1: none of its types)
+    static int type_of(const at::Tensor &t) {
+        switch (t.scalar_type()) {
+            case at::kBFloat16: return DVDQ_BF16;
+            case at::kHalf: return DVDQ_FP16;
+            case at::kFloat: return DVDQ_FP32;
+            default: return -1;
+        }
     }
     void require(bool c) { ok = ok && c; }
     int64_t integer(int i) {
@@ -285,15 +330,123 @@ PyObject *gbs_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// q, k, table, positions, sections, interleaved, inverse, q_out, k_out, stream -> q_out or (q_out, k_out)
+PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 10);
+    if (!a.ok || !THPVariable_CheckExact(args[0])) Py_RETURN_NONE;
+    const int64_t dim = THPVariable_Unpack(args[0]).dim();
+    if (dim != 3 && dim != 4) Py_RETURN_NONE;
+    const at::Tensor *q = a.view(0, dim, nullptr), *k = a.view(1, dim, q, true), *table = a.tensor(2, at::kFloat), *pos = a.tensor(3, at::kInt);
+    const int type = a.ok ? Args::type_of(*q) : -1;
+    if (!a.ok || type < 0 || table->dim() != 3 || table->size(2) != 2 || table->device() != q->device() || pos->device() != q->device()) Py_RETURN_NONE;
+    int32_t sections[4];
+    int axes = 1;
+    if (!a.none(4)) {
+        if (!PyList_CheckExact(args[4]) && !PyTuple_CheckExact(args[4])) Py_RETURN_NONE;
+        axes = (int)PySequence_Fast_GET_SIZE(args[4]);
+        if (axes < 1 || axes > 4) Py_RETURN_NONE;
+        for (int i = 0; i < axes; ++i) {
+            PyObject *v = PySequence_Fast_GET_ITEM(args[4], i);
+            int overflow = 0;
+            const long s = PyLong_CheckExact(v) ? PyLong_AsLongAndOverflow(v, &overflow) : -1;
+            if (overflow || s < 0 || s > 65536) Py_RETURN_NONE;
+            sections[i] = (int32_t)s;
+        }
+    }
+    if ((args[5] != Py_True && args[5] != Py_False) || (args[6] != Py_True && args[6] != Py_False)) Py_RETURN_NONE;
+    const int64_t B = dim == 4 ? q->size(0) : 1, T = q->size(dim - 3), D = q->size(dim - 1);
+    // positions [T], [B, T], each with [axes] where sections are given
+    const int64_t tail = a.none(4) ? 0 : 1, p_dim = pos->dim() - tail;
+    if (p_dim < 1 || p_dim > 2 || (tail && pos->size(p_dim) != axes) || pos->size(p_dim - 1) != T || (p_dim == 2 && pos->size(0) != B)) Py_RETURN_NONE;
+    if (k)
+        for (int64_t i = 0; i < dim; ++i)
+            if (i != dim - 2 && k->size(i) != q->size(i)) Py_RETURN_NONE;
+    dvdq_rope_heads heads[2];
+    at::Tensor out[2];
+    for (int w = 0; w < (k ? 2 : 1); ++w) {
+        const at::Tensor &x = w ? *k : *q;
+        out[w] = a.output_like(7 + w, x.sizes(), x);
+        if (!a.ok) Py_RETURN_NONE;
+        heads[w] = {x.data_ptr(), out[w].data_ptr(), x.size(dim - 2),
+                    {dim == 4 ? x.stride(0) : 0, x.stride(dim - 3), x.stride(dim - 2)},
+                    {dim == 4 ? out[w].stride(0) : 0, out[w].stride(dim - 3), out[w].stride(dim - 2)}};
+    }
+    void *stream = a.stream(9);
+    if (!a.ok) Py_RETURN_NONE;
+    const int rc = unlocked([&] {
+        return p_rope(&heads[0], k ? &heads[1] : nullptr, B, T, D, (const float *)table->data_ptr(), table->size(0), 2 * table->size(1),
+                      (const int32_t *)pos->data_ptr(), p_dim == 2 && B > 1 ? T * axes : 0, axes, a.none(4) ? nullptr : sections,
+                      (args[5] == Py_True ? DVDQ_ROPE_INTERLEAVED : 0) | (args[6] == Py_True ? DVDQ_ROPE_INVERSE : 0), type, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    if (k) return Py_BuildValue("(NN)", object(args[7], out[0]), object(args[8], out[1]));
+    return object(args[7], out[0]);
+    END_HANDLE_TH_ERRORS
+}
+
+// x, w, bias, act, gate, residual, y, workspace, stream -> y
+PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 9);
+    const at::Tensor *x = a.view(0, 2, nullptr), *w = a.view(1, 2, x), *bias = a.view(2, 1, x, true), *res = a.view(5, 2, x, true);
+    const int act = a.small(3);
+    const at::Tensor *gate = nullptr;
+    if (a.ok && !a.none(4)) gate = a.view(4, THPVariable_CheckExact(args[4]) && THPVariable_Unpack(args[4]).dim() == 1 ? 1 : 2, x);
+    const int type = a.ok ? Args::type_of(*x) : -1;
+    if (!a.ok || (type != DVDQ_BF16 && type != DVDQ_FP16)) Py_RETURN_NONE;
+    const int64_t M = x->size(0), K = x->size(1), N = w->size(0);
+    if (w->size(1) != K || (bias && bias->size(0) != N) || (gate && gate->size(gate->dim() - 1) != N) || (res && (res->size(0) != M || res->size(1) != N)))
+        Py_RETURN_NONE;
+    const at::Tensor y = a.output_like(6, {M, N}, *x);
+    const at::Tensor ws = a.scratch(7, a.none(7) ? p_linear_workspace_bytes(M, N, K) : 0, *x);
+    void *stream = a.stream(8);
+    if (!a.ok) Py_RETURN_NONE;
+    const int64_t gate_rows = gate ? (gate->dim() == 1 ? 1 : gate->size(0)) : 0;
+    const int rc = unlocked([&] {
+        return p_linear(x->data_ptr(), x->stride(0), w->data_ptr(), w->stride(0), ptr(bias), act, ptr(gate), gate_rows, gate_rows > 1 ? gate->stride(0) : N,
+                        ptr(res), res ? res->stride(0) : 0, M, N, K, type, y.data_ptr(), y.stride(0), ws.defined() ? ws.data_ptr() : nullptr,
+                        ws.defined() ? (size_t)ws.numel() : 0, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return object(args[6], y);
+    END_HANDLE_TH_ERRORS
+}
+
+// x, groups, weight, bias, eps, act, y, workspace, stream -> y.  [B, S, C] only: tensors of more dimensions are handed back.
+PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 9);
+    const at::Tensor *x = a.view(0, 3, nullptr), *weight = a.view(2, 1, x, true), *bias = a.view(3, 1, x, true);
+    const int64_t groups = a.integer(1);
+    const int act = a.small(5), type = a.ok ? Args::type_of(*x) : -1;
+    if (!a.ok || type < 0 || !PyFloat_CheckExact(args[4])) Py_RETURN_NONE;
+    const int64_t B = x->size(0), S = x->size(1), C = x->size(2);
+    if ((weight && weight->size(0) != C) || (bias && bias->size(0) != C)) Py_RETURN_NONE;
+    const at::Tensor y = a.output_like(6, x->sizes(), *x);
+    const at::Tensor ws = a.scratch(7, a.none(7) ? p_group_norm_workspace_bytes(B, S, C, groups) : 0, *x);
+    void *stream = a.stream(8);
+    if (!a.ok) Py_RETURN_NONE;
+    const float eps = (float)PyFloat_AS_DOUBLE(args[4]);
+    const int rc = unlocked([&] {
+        return p_group_norm(x->data_ptr(), B, S, C, x->stride(0), x->stride(1), groups, ptr(weight), ptr(bias), eps, act, type, y.data_ptr(),
+                            y.stride(0), y.stride(1), ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? (size_t)ws.numel() : 0, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return object(args[6], y);
+    END_HANDLE_TH_ERRORS
+}
+
 // torch._C._cuda_getDevice and _cuda_getCurrentRawStream, then the addresses of the C functions in the library that the binding has
 // loaded, in this order.
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
     void **const to[] = {(void **)&p_rotate_quant, (void **)&p_rotate_quant_blockwise, (void **)&p_w4ax_gemm, (void **)&p_qlinear,
                          (void **)&p_gbs_reset, (void **)&p_gbs_step, (void **)&p_codes_bytes, (void **)&p_qlinear_workspace_bytes,
-                         (void **)&p_w4_native_bytes, (void **)&p_w4_native_fp6_bytes};
+                         (void **)&p_w4_native_bytes, (void **)&p_w4_native_fp6_bytes, (void **)&p_rope, (void **)&p_linear,
+                         (void **)&p_linear_workspace_bytes, (void **)&p_group_norm, (void **)&p_group_norm_workspace_bytes};
     constexpr Py_ssize_t kFunctions = sizeof(to) / sizeof(to[0]);
     if (n != 2 + kFunctions) {
-        PyErr_SetString(PyExc_TypeError, "bind: two callables and ten addresses");
+        PyErr_SetString(PyExc_TypeError, "bind: two callables and fifteen addresses");
         return nullptr;
     }
     Py_INCREF(args[0]);
@@ -309,7 +462,8 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
 
 #define DVDQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DVDQ_METHOD(bind), DVDQ_METHOD(qlinear), DVDQ_METHOD(rotate_quant), DVDQ_METHOD(rotate_quant_blockwise),
-                         DVDQ_METHOD(w4ax_gemm), DVDQ_METHOD(gbs_reset), DVDQ_METHOD(gbs_step), {nullptr, nullptr, 0, nullptr}};
+                         DVDQ_METHOD(w4ax_gemm), DVDQ_METHOD(gbs_reset), DVDQ_METHOD(gbs_step), DVDQ_METHOD(rope), DVDQ_METHOD(linear),
+                         DVDQ_METHOD(group_norm), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
