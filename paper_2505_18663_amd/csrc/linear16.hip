@@ -404,13 +404,15 @@ constexpr int kShapeAny = 2;   // linear_any's
 
 struct LinearPlan { int shape, splits, slices, group_n; size_t parts_bytes; };
 
-// Estimated time of a shape of tile and a number of parts of K, in us.  A slice takes a workgroup 0.27 us and 0.75 us per 64 KB of it, or, where
-// its compute unit is busy, its share of the loads (162 GB/s for one compute unit alone, 74 where all of them load) and of the matrix
-// cores (1.44 us for 256 x 256 x 64).  A round of tiles has 0.6 us and 4.7 us per 256 x 256 of outputs beside its slices, 6.3 where one workgroup
-// has the compute unit for itself and nothing hides its outputs.  Parts of K are written and read back at 11.5 TB/s (they stay in the caches),
-// by a launch of 2.6 us.  The constants are fitted to some 1000 timings of 68 outputs (32 to 118800 tokens, 64 to 11384 channels, K 64 to 13824)
-// with every shape and 1 to 12 parts: the choice takes 5 % longer than the best of them in the mean, 52 % at most; always 128 x 128 without parts
-// 50 % in the mean, 7.6 times at most.
+// Estimated time of a shape of tile and a number of parts of K, in us.  A slice takes a workgroup 0.29 us and 0.48 us per 64 KB of it (1.58
+// times that where rows do not begin at a multiple of 128 bytes) or, where its compute unit is busy, its share of the loads (267 GB/s for one
+// compute unit alone, 90 where all of them load) and of the matrix cores (1.13 us for 256 x 256 x 64), and 0.13 us per 256 x 256 of outputs.  A
+// round of tiles has 1.3 us and 3.7 us per 256 x 256 of outputs beside its slices, 6.7 where one workgroup has the compute unit for itself and nothing
+// hides its outputs.  Parts of K are written and read back at 7.5 TB/s (they stay in the caches), by a launch of 2 us.  The constants are
+// fitted to some 1000 timings of 68 outputs (32 to 118800 tokens, 64 to 11384 channels, K 64 to 13824) with every shape and 1 to 12 parts:
+// the choice takes 5 % longer than the best of them in the mean, 24 % at most; always 128 x 128 without parts 50 % in the mean, 7.6 times at most.
+// 256 x 256 only where there is more than one round of it, which the estimate does not tell (1560 x 1536 x 8960 76 us, 256 x 128 50; 2000 x 13824
+// x 2000 in four parts 102 and 103).
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
     const int total = (int)((K + 63) / 64);
     LinearPlan best = {};
@@ -426,13 +428,15 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
             if (want > 1 && (per < 4 || splits == 1 || tiles * splits > slots)) break;
             const int64_t items = tiles * splits, full = items / slots;
             const int rest = (int)(items - full * slots);
-            const float load = bytes * (1 / 162e3f + (items < 256 ? (float)items / 256 : 1.0f) / 138e3f), lone = 0.27f + 0.75f / 65536 * bytes;
+            if (i == 0 && items <= 256) continue;
+            const float load = bytes * (1 / 267e3f + (items < 256 ? (float)items / 256 : 1.0f) / 135e3f);
+            const float lone = 0.29f + (K % 64 == 0 ? 0.48f : 0.76f) / 65536 * bytes;
             auto round = [&](int resident) {
-                return 0.6f + (4.7f * (float)resident + (sh.per_cu == 1 ? 1.6f : 0.0f)) * area +
-                       (float)per * std::max(lone, (float)resident * std::max(load, 1.44f * area));
+                return 1.3f + (3.7f * (float)resident + (sh.per_cu == 1 ? 3.0f : 0.0f)) * area +
+                       (float)per * (std::max(lone, (float)resident * std::max(load, 1.13f * area)) + 0.13f * (float)resident * area);
             };
             float time = (float)full * round(sh.per_cu) + (rest ? round((rest + 255) / 256) : 0.0f);
-            if (splits > 1) time += 2.6f + (float)items * area * (8 * 65536 / 11.5e6f);
+            if (splits > 1) time += 2.0f + (float)items * area * (8 * 65536 / 7.5e6f);
             if (time < best_time) {
                 best_time = time;
                 const int groups = (n_tiles + 5) / 6;   // columns of tiles that are run through before the next row
