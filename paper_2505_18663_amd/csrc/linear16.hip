@@ -245,7 +245,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
     // at the same time share panels, and so do those of the next round (as interleaved rounds of the whole chip, 32760 x 13824 x 5120
     // took 3340 us in place of 3190).
     const int xcds = min(8, grid), xcd = blockIdx.x % xcds, step = (grid - xcd + xcds - 1) / xcds;
-    const int end = (int)((int64_t)items * (xcd + 1) / xcds);
+    const int share = items / xcds, more = items % xcds;     // (the first XCDs have one more, of workgroups as well as of tiles)
+    const int end = share * (xcd + 1) + min(xcd + 1, more);
     const uint32_t lds_w = lds_address(lds) + wave * (1024 * LW), lds_x = lds_address(lds) + 3 * kUnitW + wave * (1024 * LX);
     const uint8_t *src_w, *src_x;
     uint32_t off_w[LW], off_x[LX];
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
         for (int f = 0; f < FH; ++f) fx[p & 1][f] = lds[sx * (kUnitX / 16) + (at_x ^ (4 * ks)) + 128 * (h * FH + f)];
     };
 
-    int t = (int)((int64_t)items * xcd / xcds) + blockIdx.x / xcds, sw = 0, sx = 0;   // places of the present slice
+    int t = share * xcd + min(xcd, more) + blockIdx.x / xcds, sw = 0, sx = 0;   // places of the present slice
     if (t >= end) return;
     aim(t);
     load_w(0, 0, false);
@@ -404,17 +405,17 @@ constexpr int kShapeAny = 2;   // linear_any's
 
 struct LinearPlan { int shape, splits, slices, group_n; size_t parts_bytes; };
 
-// Estimated time of a shape of tile and a number of parts of K, in us.  A slice takes a workgroup 0.29 us and 0.48 us per 64 KB of it (1.58
-// times that where rows do not begin at a multiple of 128 bytes) or, where its compute unit is busy, its share of the loads (267 GB/s for one
-// compute unit alone, 90 where all of them load) and of the matrix cores (1.13 us for 256 x 256 x 64), and 0.13 us per 256 x 256 of outputs.  A
-// round of tiles has 1.3 us and 3.7 us per 256 x 256 of outputs beside its slices, 6.7 where one workgroup has the compute unit for itself and nothing
-// hides its outputs.  Parts of K are written and read back at 7.5 TB/s (they stay in the caches), by a launch of 2 us.  The constants are
-// fitted to some 1000 timings of 68 outputs (32 to 118800 tokens, 64 to 11384 channels, K 64 to 13824) with every shape and 1 to 12 parts:
-// the choice takes 5 % longer than the best of them in the mean, 24 % at most; always 128 x 128 without parts 50 % in the mean, 7.6 times at most.
-// 256 x 256 only where there is more than one round of it, which the estimate does not tell (1560 x 1536 x 8960 76 us, 256 x 128 50; 2000 x 13824
-// x 2000 in four parts 102 and 103).
+// Estimated time of a shape of tile and a number of parts of K, in us.  A slice takes a workgroup 0.34 us and 0.23 us per 64 KB of it (1.85
+// times that where rows do not begin at a multiple of 128 bytes) or, where its compute unit is busy, its share of the loads (275 GB/s for one
+// compute unit alone, 74 where all of them load, 13 % less with such rows) and of the matrix cores (1.19 us for 256 x 256 x 64), and 0.1 us
+// per 256 x 256 of outputs.  A round of tiles has 1.6 us and 0.4 us per 256 x 256 of outputs beside its slices, 6.2 where one workgroup has the
+// compute unit for itself and nothing hides its outputs.  Parts of K are written and read back at 9.2 TB/s (they stay in the caches), by a
+// launch of 3.2 us.  The constants are fitted to 818 timings of 67 outputs (32 to 118800 tokens, 64 to 11384 channels, K 64 to 13824) with every shape
+// and 1 to 12 parts: the choice takes 2 % longer than the best of them in the mean, 13 % at most; always 128 x 128 without parts
+// 35 % in the mean, 6.2 times at most.
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
     const int total = (int)((K + 63) / 64);
+    const bool lines = K % 64 == 0;
     LinearPlan best = {};
     float best_time = 1e30f;
     for (int i = 0; i < (int)(sizeof(kShapes) / sizeof(kShapes[0])); ++i) {
@@ -428,15 +429,14 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
             if (want > 1 && (per < 4 || splits == 1 || tiles * splits > slots)) break;
             const int64_t items = tiles * splits, full = items / slots;
             const int rest = (int)(items - full * slots);
-            if (i == 0 && items <= 256) continue;
-            const float load = bytes * (1 / 267e3f + (items < 256 ? (float)items / 256 : 1.0f) / 135e3f);
-            const float lone = 0.29f + (K % 64 == 0 ? 0.48f : 0.76f) / 65536 * bytes;
+            const float load = bytes * (lines ? 1.0f : 1.15f) * (1 / 275e3f + (items < 256 ? (float)items / 256 : 1.0f) / 100e3f);
+            const float lone = 0.34f + (lines ? 0.23f : 0.43f) / 65536 * bytes;
             auto round = [&](int resident) {
-                return 1.3f + (3.7f * (float)resident + (sh.per_cu == 1 ? 3.0f : 0.0f)) * area +
-                       (float)per * (std::max(lone, (float)resident * std::max(load, 1.13f * area)) + 0.13f * (float)resident * area);
+                return 1.6f + (0.4f * (float)resident + (sh.per_cu == 1 ? 5.7f : 0.0f)) * area +
+                       (float)per * (std::max(lone, (float)resident * std::max(load, 1.19f * area)) + 0.1f * (float)resident * area);
             };
             float time = (float)full * round(sh.per_cu) + (rest ? round((rest + 255) / 256) : 0.0f);
-            if (splits > 1) time += 2.0f + (float)items * area * (8 * 65536 / 7.5e6f);
+            if (splits > 1) time += 3.2f + (float)items * area * (8 * 65536 / 9.2e6f);
             if (time < best_time) {
                 best_time = time;
                 const int groups = (n_tiles + 5) / 6;   // columns of tiles that are run through before the next row
