@@ -188,6 +188,22 @@ __global__ __launch_bounds__(256, 2) void linear_any(LinearArgs a) {
     else epilogue<E, ACT>(a, acc, __builtin_amdgcn_readfirstlane(m0 + wm), __builtin_amdgcn_readfirstlane(n0 + wn));
 }
 
+// Rows of K elements at any address -> rows of `pitch` elements, a multiple of 64, zero past K: activations (rows_x of them), then weights.
+template <typename E>
+__global__ __launch_bounds__(256) void linear_pad(const uint16_t *x, int64_t ldx, int rows_x, const uint16_t *w, int64_t ldw, int rows_w, int K,
+                                                  int pitch, uint16_t *out) {
+    const uint32_t pieces = (uint32_t)pitch / 8;
+    const int64_t total = (int64_t)(rows_x + rows_w) * pieces;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += gridDim.x * (int64_t)256) {
+        const int64_t row = i / pieces;
+        const int k = (int)(i - row * pieces) * 8;
+        const uint16_t *src = row < rows_x ? x + row * ldx : w + (row - rows_x) * ldw;
+        Piece<E> p = {};
+        if (k < K) p = load_piece<E>(src + k, min(8, K - k));
+        reinterpret_cast<uint4 *>(out)[i] = __builtin_bit_cast(uint4, p);
+    }
+}
+
 // Joins the parts of K, in their order, and finishes: a wave per 64 channels x 16 tokens of tiles of WN x WM waves of 64 channels x 16 FM tokens.
 template <typename E, int ACT>
 __global__ __launch_bounds__(256) void linear_join(LinearArgs a, int FM, int WN, int WM, int group_n) {
@@ -403,7 +419,7 @@ struct Shape { int fm, wn, wm, per_cu; };
 constexpr Shape kShapes[] = {{8, 4, 2, 1}, {4, 4, 2, 1}, {4, 2, 2, 2}, {2, 2, 2, 2}, {2, 1, 2, 4}};
 constexpr int kShapeAny = 2;   // linear_any's
 
-struct LinearPlan { int shape, splits, slices, group_n; size_t parts_bytes; };
+struct LinearPlan { int shape, splits, slices, group_n; size_t parts_bytes, pad_bytes; float time; };
 
 // Estimated time of a shape of tile and a number of parts of K, in us.  A slice takes a workgroup 0.34 us and 0.23 us per 64 KB of it (1.85
 // times that where rows do not begin at a multiple of 128 bytes) or, where its compute unit is busy, its share of the loads (275 GB/s for one
@@ -417,7 +433,7 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
     const int total = (int)((K + 63) / 64);
     const bool lines = K % 64 == 0;
     LinearPlan best = {};
-    float best_time = 1e30f;
+    best.time = 1e30f;
     for (int i = 0; i < (int)(sizeof(kShapes) / sizeof(kShapes[0])); ++i) {
         if (any && i != kShapeAny) continue;
         const Shape &sh = kShapes[i];
@@ -437,15 +453,25 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
             };
             float time = (float)full * round(sh.per_cu) + (rest ? round((rest + 255) / 256) : 0.0f);
             if (splits > 1) time += 3.2f + (float)items * area * (8 * 65536 / 9.2e6f);
-            if (time < best_time) {
-                best_time = time;
+            if (any) time *= 1.7f;
+            if (time < best.time) {
                 const int groups = (n_tiles + 5) / 6;   // columns of tiles that are run through before the next row
-                best = {i, splits, per, any ? n_tiles : (n_tiles + groups - 1) / groups, splits > 1 ? (size_t)(items * bn * bm) * sizeof(float) : 0};
+                best = {i, splits, per, any ? n_tiles : (n_tiles + groups - 1) / groups, splits > 1 ? (size_t)(items * bn * bm) * sizeof(float) : 0, 0, time};
             }
         }
     }
+    // Rows that are no whole pieces: copied into ones that are, where that takes less than what linear_any loses (its registers on the way to
+    // LDS cost it 1.4 to 1.9 times the time of 128 x 128 tiles: 32760 x 1533 x 8960 1655 us, copied 812).
+    if (any && K % 8 != 0) {
+        const int64_t pitch = (K + 63) / 64 * 64;
+        LinearPlan p = linear_plan(M, N, pitch, false);
+        p.pad_bytes = (size_t)((M + N) * pitch) * 2;
+        p.time += 3.0f + (float)p.pad_bytes * (2 / 5e6f);
+        if (p.time < best.time) return p;
+    }
     return best;
 }
+inline size_t plan_bytes(const LinearPlan &p) { return (p.pad_bytes + 255) / 256 * 256 + p.parts_bytes; }
 
 template <typename E, int ACT>
 int launch_product(const LinearArgs &a, const LinearPlan &p, bool any, hipStream_t stream) {
@@ -468,8 +494,8 @@ int launch_product(const LinearArgs &a, const LinearPlan &p, bool any, hipStream
 }  // namespace
 
 size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-    const size_t any = linear_plan(M, N, K, true).parts_bytes;   // (addresses and pitches are not known here)
-    return K % 8 == 0 ? std::max(any, linear_plan(M, N, K, false).parts_bytes) : any;
+    const size_t any = plan_bytes(linear_plan(M, N, K, true));   // (addresses and pitches are not known here)
+    return K % 8 == 0 ? std::max(any, plan_bytes(linear_plan(M, N, K, false))) : any;
 }
 
 int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias, int act, const void *gate, int64_t gate_rows,
@@ -482,9 +508,20 @@ int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const 
     a.M = (int)M, a.N = (int)N, a.K = (int)K;
     a.gate_rows = gate ? (int)(M / gate_rows) : 1;
     const auto whole = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 7) == 0 && ld < (int64_t)1 << 22; };
-    const bool any = K % 8 != 0 || !whole(x, M > 1 ? ldx : 0) || !whole(w, N > 1 ? ldw : 0);
+    bool any = K % 8 != 0 || !whole(x, M > 1 ? ldx : 0) || !whole(w, N > 1 ? ldw : 0);
     const LinearPlan p = linear_plan(M, N, K, any);
-    a.parts = static_cast<float4 *>(workspace);
+    a.parts = reinterpret_cast<float4 *>(static_cast<uint8_t *>(workspace) + (p.pad_bytes + 255) / 256 * 256);
+    if (p.pad_bytes) {
+        const int pitch = (int)((K + 63) / 64 * 64);
+        uint16_t *rows = static_cast<uint16_t *>(workspace);
+        const int64_t blocks = std::min((int64_t)256 * 32, ((M + N) * (pitch / 8) + 255) / 256);
+        linear_pad<Bf16><<<dim3((unsigned)blocks), 256, 0, stream>>>(a.x, ldx, a.M, a.w, ldw, a.N, a.K, pitch, rows);   // (bits: any 16-bit type)
+        const int rc = check_launch();
+        if (rc != DVDQ_OK) return rc;
+        a.x = rows, a.w = rows + M * pitch;
+        a.ldx = a.ldw = a.K = pitch;
+        any = false;
+    }
     a.splits = p.splits;
     a.slices = p.slices;
     return with_type(dtype, [&](auto type) {
