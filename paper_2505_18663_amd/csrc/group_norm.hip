@@ -27,7 +27,7 @@ struct GnArgs {
     int64_t slab_rows;                        // rows of a part
     int slabs;
     float eps;
-    Moments *parts;                           // [B][slabs][groups]
+    Moments *parts;                           // [B][groups][slabs]
     float2 *stats;                            // [B][groups]: mean, 1 / sqrt(var + eps)
 };
 
@@ -43,22 +43,25 @@ static __device__ __forceinline__ void join(float n, float (&mean)[V], float (&m
     }
 }
 
-constexpr int kBatch = 8;   // rows of a thread that are in registers at a time
+constexpr int kBatch = 4;   // rows of a thread that are in registers at a time
 
-template <typename E>
+// WHOLE: a piece lies within one group (C / groups a multiple of it), and a thread joins its channels before it meets the others;
+// otherwise channels are joined first.
+template <typename E, bool WHOLE>
 __global__ __launch_bounds__(1024) void gn_parts(GnArgs a) {
     using Raw = typename E::Raw;
     constexpr int V = E::kVec;
-    extern __shared__ float lds[];                      // [rows_at_once][2][cols * V]
+    extern __shared__ float lds[];                      // WHOLE: [rows_at_once][cols] moments, else [rows_at_once][2][cols * V]
     const int b = blockIdx.y, slab = blockIdx.x;
     const int64_t s0 = slab * a.slab_rows;
     const int rows = (int)min(a.S - s0, a.slab_rows);
     const int width = a.cols * V;
     const int r = threadIdx.x / a.cols, col = threadIdx.x - r * a.cols, c0 = col * V, n = min(V, a.C - c0);
     const int64_t step = a.rows_at_once * a.x_row;
+    const auto rows_of = [&](int i) { return max(0, (rows - i + a.rows_at_once - 1) / a.rows_at_once); };   // of the i-th row of threads
     if (r < a.rows_at_once) {
         const Raw *x = static_cast<const Raw *>(a.x) + (b * a.x_batch + (s0 + r) * a.x_row + c0);
-        const int mine = (rows - r + a.rows_at_once - 1) / a.rows_at_once;   // rows of this thread (0 or less: none)
+        const int mine = rows_of(r);
         float mean[V] = {}, m2[V] = {};
         for (int i0 = 0; i0 < mine; i0 += kBatch) {
             const int nb = min(kBatch, mine - i0);
@@ -90,39 +93,76 @@ __global__ __launch_bounds__(1024) void gn_parts(GnArgs a) {
                 }
             join<V>((float)i0, mean, m2, (float)nb, mb, qb);
         }
+        if constexpr (WHOLE) {
+            float sum = 0.0f, m = 0.0f;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            lds[(2 * r) * width + c0 + j] = mean[j];
-            lds[(2 * r + 1) * width + c0 + j] = m2[j];
+            for (int j = 1; j < V; ++j) sum += mean[j] - mean[0];
+            const float all = fmaf(sum, 1.0f / V, mean[0]);
+#pragma unroll
+            for (int j = 0; j < V; ++j) m += fmaf((mean[j] - all) * (mean[j] - all), (float)mine, m2[j]);
+            reinterpret_cast<Moments *>(lds)[r * a.cols + col] = {all, m};
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                lds[(2 * r) * width + c0 + j] = mean[j];
+                lds[(2 * r + 1) * width + c0 + j] = m2[j];
+            }
         }
     }
     __syncthreads();
-    // per channel: mean and squared deviations over the slab, in the first two rows of lds
-    for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
-        const float first = lds[c];
-        float sum = 0.0f, m2 = 0.0f;
-        for (int i = 1; i < a.rows_at_once; ++i) sum = fmaf((float)max(0, (rows - i + a.rows_at_once - 1) / a.rows_at_once), lds[2 * i * width + c] - first, sum);
-        const float mean = first + sum / (float)rows;
-        for (int i = 0; i < a.rows_at_once; ++i) {
-            const float d = lds[2 * i * width + c] - mean;
-            m2 += fmaf((float)max(0, (rows - i + a.rows_at_once - 1) / a.rows_at_once), d * d, lds[(2 * i + 1) * width + c]);
+    if constexpr (!WHOLE) {
+        // per channel: mean and squared deviations over the slab, in the first two rows of lds
+        for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+            const float first = lds[c];
+            float sum = 0.0f, m2 = 0.0f;
+            for (int i = 1; i < a.rows_at_once; ++i) sum = fmaf((float)rows_of(i), lds[2 * i * width + c] - first, sum);
+            const float mean = first + sum / (float)rows;
+            for (int i = 0; i < a.rows_at_once; ++i) {
+                const float d = lds[2 * i * width + c] - mean;
+                m2 += fmaf((float)rows_of(i), d * d, lds[(2 * i + 1) * width + c]);
+            }
+            lds[c] = mean;
+            lds[width + c] = m2;
         }
-        lds[c] = mean;
-        lds[width + c] = m2;
+        __syncthreads();
     }
-    __syncthreads();
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    for (int g = wave; g < a.groups; g += waves) {
-        float sum = 0.0f, m2 = 0.0f;
-        const float first = lds[g * a.cpg];
-        for (int c = lane; c < a.cpg; c += 64) sum += lds[g * a.cpg + c] - first;
-        const float mean = first + wave_sum(sum) / (float)a.cpg;
-        for (int c = lane; c < a.cpg; c += 64) {
-            const float d = lds[g * a.cpg + c] - mean;
-            m2 += fmaf((float)rows * d, d, lds[width + g * a.cpg + c]);
-        }
-        m2 = wave_sum(m2);
-        if (lane == 0) a.parts[((int64_t)b * a.slabs + slab) * a.groups + g] = {mean, m2};
+    // The groups, `lanes` lanes (a power of two) for each: entries e of a group are pieces of rows of threads, or channels.
+    const int per_row = a.cpg / V, entries = WHOLE ? a.rows_at_once * per_row : a.cpg;
+    const int lanes = entries >= 64 ? 64 : 1 << (32 - __builtin_clz(max(entries, 2) - 1)), l = threadIdx.x & (lanes - 1);
+    const auto total = [&](float v) {
+        for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o);
+        return v;
+    };
+    for (int g0 = 0; g0 < a.groups; g0 += blockDim.x / lanes) {
+        const int g = g0 + threadIdx.x / lanes;
+        if (g0 + (int)(threadIdx.x & ~63) / lanes >= a.groups) continue;   // (of whole waves only: the lanes of a wave meet in total())
+        const auto entry = [&](int e, float &weight) {
+            if constexpr (WHOLE) {
+                const int i = e / per_row;
+                weight = (float)rows_of(i) * V;
+                return reinterpret_cast<const Moments *>(lds)[i * a.cols + g * per_row + (e - i * per_row)];
+            } else {
+                weight = (float)rows;
+                return Moments{lds[g * a.cpg + e], lds[width + g * a.cpg + e]};
+            }
+        };
+        const bool valid = g < a.groups;
+        float w, sum = 0.0f, m2 = 0.0f;
+        const float first = valid ? entry(0, w).mean : 0.0f;   // (the first row of threads has rows in every slab)
+        if (valid)
+            for (int e = l; e < entries; e += lanes) {
+                const float m = entry(e, w).mean;
+                if (w > 0.0f) sum = fmaf(w, m - first, sum);
+            }
+        const float mean = first + total(sum) / ((float)rows * (float)a.cpg);
+        if (valid)
+            for (int e = l; e < entries; e += lanes) {
+                const Moments m = entry(e, w);
+                const float d = m.mean - mean;
+                if (w > 0.0f) m2 += fmaf(w * d, d, m.m2);
+            }
+        m2 = total(m2);
+        if (valid && l == 0) a.parts[((int64_t)b * a.groups + g) * a.slabs + slab] = {mean, m2};
     }
 }
 
@@ -142,13 +182,13 @@ constexpr int kMaxSlabs = 2048, kPerThread = kMaxSlabs / 256;
 __global__ __launch_bounds__(256) void gn_join(GnArgs a) {
     __shared__ double lds[2][4];
     const int g = blockIdx.x, b = blockIdx.y;
-    const Moments *p = a.parts + (int64_t)b * a.slabs * a.groups + g;
+    const Moments *p = a.parts + ((int64_t)b * a.groups + g) * a.slabs;
     Moments m[kPerThread];
     double rows[kPerThread], sum = 0.0, m2 = 0.0;
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
         const int slab = threadIdx.x + 256 * i;
-        if (slab < a.slabs) m[i] = p[(int64_t)slab * a.groups];
+        if (slab < a.slabs) m[i] = p[slab];
         else m[i] = {};
         rows[i] = slab < a.slabs ? (double)min(a.S - slab * a.slab_rows, a.slab_rows) : 0.0;
     }
@@ -317,7 +357,10 @@ int launch_group_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_
             one_launch(std::integral_constant<int, 2>()) || one_launch(std::integral_constant<int, 1>()))
             return check_launch();
         const dim3 grid(p.slabs, (unsigned)B);
-        gn_parts<E><<<grid, p.threads, (size_t)p.rows_at_once * 2 * p.cols * E::kVec * sizeof(float), stream>>>(a);
+        if (a.cpg % E::kVec == 0)
+            gn_parts<E, true><<<grid, p.threads, (size_t)p.rows_at_once * p.cols * sizeof(Moments), stream>>>(a);
+        else
+            gn_parts<E, false><<<grid, p.threads, (size_t)p.rows_at_once * 2 * p.cols * E::kVec * sizeof(float), stream>>>(a);
         gn_join<<<dim3((unsigned)groups, (unsigned)B), 256, 0, stream>>>(a);
         const bool stream_out = (int64_t)B * S * C * (int64_t)sizeof(typename E::Raw) >= (4 << 20);
         const auto apply = silu ? (stream_out ? gn_apply<E, DVDQ_ACT_SILU, true> : gn_apply<E, DVDQ_ACT_SILU, false>)
