@@ -188,6 +188,86 @@ __global__ __launch_bounds__(256, 2) void linear_any(LinearArgs a) {
     else epilogue<E, ACT>(a, acc, __builtin_amdgcn_readfirstlane(m0 + wm), __builtin_amdgcn_readfirstlane(n0 + wn));
 }
 
+// ---- few tokens (at most 16): bound by the weights, which are read once, straight into registers
+// A workgroup has 16 channels, its waves parts of K: a lane reads 32 bytes of a channel (the four lanes of a channel a whole line) and the same part of its
+// token, two matrix instructions' worth, twice over before the first product; the waves' sums meet in LDS in their order.
+// (The instruction's order of K does not matter as long as it is the same on both sides.)
+// 2 x 1536 x 9216, 28 MB of weights: 8.9 us with 8 waves, 12.8 with 16, 9.9 with 4; as tiles 14.0.  1 x 1536 x 4608 6.8 and 11.9, 16 x 1536 x 13824
+// 14.9 and 17.9, 2 x 5120 x 30720 57 and 66.  Few channels leave compute units idle and long rows their waves with too little in flight:
+// 8 x 13824 x 128 22 and 14, 16 x 5120 x 5120 23 and 19, 2 x 13824 x 5120 36 and 36; these are tiles.
+constexpr int kFewWaves = 8;
+inline bool few_tokens(int64_t M, int64_t N, int64_t K) { return M <= 16 && (K <= 4096 || N >= 16384); }
+template <typename E, int ACT>
+__global__ __launch_bounds__(512) void linear_few(LinearArgs a) {
+    extern __shared__ uint4 lds[];
+    float *sums = reinterpret_cast<float *>(lds);            // [wave][token][channel]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, n0 = blockIdx.x * 16;
+    const uint16_t *w = a.w + min(n0 + (lane & 15), a.N - 1) * a.ldw, *x = a.x + min(lane & 15, a.M - 1) * a.ldx;
+    const int steps = (a.K + 63) >> 6, q0 = (int)((int64_t)steps * wave / waves), q1 = (int)((int64_t)steps * (wave + 1) / waves);
+    constexpr int AHEAD = 2;
+    v4f acc[2] = {};
+    const auto multiply = [&](const Piece<E> &pw, const Piece<E> &px, int h) {
+        acc[h] = mfma<E>(__builtin_bit_cast(uint4, pw), __builtin_bit_cast(uint4, px), acc[h]);
+    };
+    const int whole = min(q1, a.K >> 6);                     // steps of 64 elements that there are
+    w += (lane >> 4) * 16, x += (lane >> 4) * 16;
+    int q = q0;
+    for (; q + AHEAD <= whole; q += AHEAD) {
+        Piece<E> pw[AHEAD][2], px[AHEAD][2];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                pw[i][h] = load_piece<E>(w + (q + i) * 64 + 8 * h, 8);
+                px[i][h] = load_piece<E>(x + (q + i) * 64 + 8 * h, 8);
+            }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) multiply(pw[i][h], px[i][h], h);
+    }
+    if (q < whole) {                                         // fewer than AHEAD: the rest once more, as nothing
+        Piece<E> pw[AHEAD - 1][2], px[AHEAD - 1][2];
+#pragma unroll
+        for (int i = 0; i < AHEAD - 1; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                pw[i][h] = load_piece<E>(w + min(q + i, whole - 1) * 64 + 8 * h, 8);
+                px[i][h] = load_piece<E>(x + min(q + i, whole - 1) * 64 + 8 * h, 8);
+            }
+#pragma unroll
+        for (int i = 0; i < AHEAD - 1; ++i)
+            if (q + i < whole) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) multiply(pw[i][h], px[i][h], h);
+            }
+    }
+    if (whole < q1) {                                        // the last step, of fewer than 64 elements
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = whole * 64 + 8 * h, left = a.K - k - (lane >> 4) * 16;
+            Piece<E> pw = {}, px = {};
+            if (left > 0) {
+                pw = load_piece<E>(w + k, left);
+                px = load_piece<E>(x + k, left);
+            }
+            multiply(pw, px, h);
+        }
+    }
+    const v4f sum = acc[0] + acc[1];
+    reinterpret_cast<v4f *>(sums)[(wave * 16 + (lane & 15)) * 4 + (lane >> 4)] = sum;
+    __syncthreads();
+    const int m = threadIdx.x >> 4, n = n0 + (threadIdx.x & 15);
+    if (threadIdx.x >= 256 || m >= a.M || n >= a.N) return;
+    float v = 0.0f;
+    for (int i = 0; i < waves; ++i) v += sums[i * 256 + threadIdx.x];
+    if (a.bias) v += E::to_f32(a.bias[n]);
+    v = activate<ACT>(v);
+    if (a.gate) v *= E::to_f32(a.gate[(m / a.gate_rows) * a.ldg + n]);
+    if (a.residual) v += E::to_f32(a.residual[m * a.ldr + n]);
+    a.y[m * a.ldy + n] = E::from_f32(v);
+}
+
 // Rows of K elements at any address -> rows of `pitch` elements, a multiple of 64, zero past K: activations (rows_x of them), then weights.
 template <typename E>
 __global__ __launch_bounds__(256) void linear_pad(const uint16_t *x, int64_t ldx, int rows_x, const uint16_t *w, int64_t ldw, int rows_w, int K,
@@ -494,6 +574,7 @@ int launch_product(const LinearArgs &a, const LinearPlan &p, bool any, hipStream
 }  // namespace
 
 size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    if (few_tokens(M, N, K)) return 0;
     const size_t any = plan_bytes(linear_plan(M, N, K, true));   // (addresses and pitches are not known here)
     return K % 8 == 0 ? std::max(any, plan_bytes(linear_plan(M, N, K, false))) : any;
 }
@@ -508,6 +589,19 @@ int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const 
     a.M = (int)M, a.N = (int)N, a.K = (int)K;
     a.gate_rows = gate ? (int)(M / gate_rows) : 1;
     const auto whole = [](const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 7) == 0 && ld < (int64_t)1 << 22; };
+    if (few_tokens(M, N, K))
+        return with_type(dtype, [&](auto type) {
+            using E = decltype(type);
+            if constexpr (sizeof(typename E::Raw) == 2) {
+                return with_act(act, [&](auto which) {
+                    constexpr int ACT = decltype(which)::value;
+                    linear_few<E, ACT><<<dim3((unsigned)((N + 15) / 16)), 64 * kFewWaves, kFewWaves * 1024, stream>>>(a);
+                    return check_launch();
+                });
+            } else {
+                return (int)DVDQ_ERR_UNSUPPORTED;
+            }
+        });
     bool any = K % 8 != 0 || !whole(x, M > 1 ? ldx : 0) || !whole(w, N > 1 ? ldw : 0);
     const LinearPlan p = linear_plan(M, N, K, any);
     a.parts = reinterpret_cast<float4 *>(static_cast<uint8_t *>(workspace) + (p.pad_bytes + 255) / 256 * 256);
