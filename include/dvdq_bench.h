@@ -87,6 +87,13 @@ int dvdq_bench_fill_tile_counters(uint32_t value, void *hip_stream);
  * Process-wide (an atomic that every launch reads once). */
 int dvdq_bench_set_gbs_wait(int64_t ticks);
 
+/*
+ * How dvdq_linear takes a product whose operands have whole 16-byte pieces (`any` = 0) or not (1): -1 for few tokens straight from
+ * the weights, else the shape of tile (0: 256 x 256 .. 4: 64 x 64) + 16 * parts of K, + 4096 where the rows are copied first, + 8192 where
+ * they go through registers.  Host only.
+ */
+int dvdq_bench_linear_choice(int64_t M, int64_t N, int64_t K, int any);
+
 #ifdef __cplusplus
 }
 #endif

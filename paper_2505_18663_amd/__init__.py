@@ -39,7 +39,7 @@ EXPORTED_SYMBOLS = (
     "dvdq_rotate_quant", "dvdq_rotate_quant_blockwise", "dvdq_w4ax_gemm", "dvdq_qlinear", "dvdq_qlinear_workspace_bytes",
     "dvdq_qlinear_scale_offset", "dvdq_qlinear_rowsum_offset", "dvdq_qlinear_static", "dvdq_static_workspace_bytes", "dvdq_w4_prepack", "dvdq_w4_native_bytes", "dvdq_w4_prepack_fp6",
     "dvdq_w4_native_fp6_bytes", "dvdq_codes_bytes", "dvdq_status_string",
-    "dvdq_version", "dvdq_rope", "dvdq_rope_table", "dvdq_linear", "dvdq_linear_workspace_bytes", "dvdq_group_norm", "dvdq_group_norm_workspace_bytes",
+    "dvdq_version", "dvdq_rope", "dvdq_rope_table", "dvdq_linear", "dvdq_linear_workspace_bytes", "dvdq_bench_linear_choice", "dvdq_group_norm", "dvdq_group_norm_workspace_bytes",
     "dvdq_gbs_workspace_bytes", "dvdq_gbs_reset", "dvdq_gbs_step", "dvdq_bgr_quantize", "dvdq_bench_copy", "dvdq_bench_mfma_i8", "dvdq_bench_mfma_fp6", "dvdq_bench_set_gemm_variant", "dvdq_bench_set_gemm_schedule", "dvdq_bench_fill_tile_counters", "dvdq_bench_set_gemm_grid_limit", "dvdq_bench_set_gbs_wait", "dvdq_bench_gemm_choice", "dvdq_bench_narrow_tiles", "dvdq_bench_quantizer_waves", "dvdq_bench_qlinear_choice", "dvdq_bench_bgr_choice", "dvdq_release_stream",
 )
 
@@ -141,6 +141,8 @@ def lib() -> C.CDLL:
     L.dvdq_linear.restype = i32
     L.dvdq_linear_workspace_bytes.argtypes = [i64, i64, i64]
     L.dvdq_linear_workspace_bytes.restype = sz
+    L.dvdq_bench_linear_choice.argtypes = [i64, i64, i64, i32]
+    L.dvdq_bench_linear_choice.restype = i32
     L.dvdq_group_norm.argtypes = [vp, i64, i64, i64, i64, i64, i64, vp, vp, C.c_float, i32, i32, vp, i64, i64, vp, sz, vp]
     L.dvdq_group_norm.restype = i32
     L.dvdq_group_norm_workspace_bytes.argtypes = [i64, i64, i64, i64]
@@ -811,6 +813,11 @@ def bench_bgr_choice(N: int, K: int, n_steps: int = 100, max_refine: int = 10) -
 def bench_qlinear_choice(M: int, N: int, K: int, x: int = 1 << 40, y: int = 1 << 41, workspace: int = 1 << 42, workspace_bytes: int = 1 << 30) -> int:
     """How qlinear runs a layer with its arguments at these addresses: 0 as two launches, 1 or 2 as one (tiles of 32 or 64 channels).  Needs no GPU."""
     return lib().dvdq_bench_qlinear_choice(x, y, workspace, workspace_bytes, M, N, K)
+
+
+def bench_linear_choice(M: int, N: int, K: int, any: bool = False) -> int:
+    """How linear takes a product (see dvdq_bench_linear_choice).  Needs no GPU."""
+    return lib().dvdq_bench_linear_choice(M, N, K, int(any))
 
 
 def bench_set_gemm_schedule(schedule: int) -> None:

@@ -1,5 +1,6 @@
 // C ABI of the operators around the quantized layer: argument validation on the host, then kernel launches.
 #include "dvdq_internal.h"
+#include "../../include/dvdq_bench.h"
 
 namespace {
 
@@ -92,6 +93,11 @@ int dvdq_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const vo
     }
     return dvdq::launch_linear(x, ldx, w, ldw, bias, act, gate, gate_rows, ldg, residual, ldr, M, N, K, dtype, y, ldy, workspace,
                                static_cast<hipStream_t>(hip_stream));
+}
+
+int dvdq_bench_linear_choice(int64_t M, int64_t N, int64_t K, int any) {
+    if (M < 1 || N < 1 || K < 1 || M > kMaxTokens || N > kMaxChannels || K > kMaxChannels) return -2;
+    return dvdq::linear_choice(M, N, K, any || K % 8 != 0);
 }
 
 size_t dvdq_group_norm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t groups) {

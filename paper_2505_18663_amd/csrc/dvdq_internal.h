@@ -166,6 +166,7 @@ int launch_rope(const dvdq_rope_heads *q, const dvdq_rope_heads *k, int64_t B, i
                 int64_t R, const int32_t *positions, int64_t pos_batch, int n_axes, const int32_t *sections, bool interleaved, bool inverse,
                 int dtype, hipStream_t stream);
 size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int linear_choice(int64_t M, int64_t N, int64_t K, bool any);
 int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias, int act, const void *gate, int64_t gate_rows,
                   int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype, void *y, int64_t ldy,
                   void *workspace, hipStream_t stream);

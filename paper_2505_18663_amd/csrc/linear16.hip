@@ -579,6 +579,12 @@ size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     return K % 8 == 0 ? std::max(any, plan_bytes(linear_plan(M, N, K, false))) : any;
 }
 
+int linear_choice(int64_t M, int64_t N, int64_t K, bool any) {
+    if (few_tokens(M, N, K)) return -1;
+    const LinearPlan p = linear_plan(M, N, K, any);
+    return p.shape + 16 * p.splits + (p.pad_bytes ? 4096 : any ? 8192 : 0);
+}
+
 int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias, int act, const void *gate, int64_t gate_rows,
                   int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype, void *y, int64_t ldy,
                   void *workspace, hipStream_t stream) {

@@ -18,7 +18,7 @@ F32 = 2.0 ** -24
 def assert_close(got, ref, slack, what):
     """|got - ref| <= one rounding + slack, elementwise; NaN where, and only where, the reference is NaN."""
     u, tiny = UNIT[got.dtype], TINY[got.dtype]
-    got, ref = got.detach().cpu().double(), ref.double()
+    got, ref = got.detach().to(ref.device).double(), ref.double()
     assert got.shape == ref.shape, (what, got.shape, ref.shape)
     nan = ref.isnan()
     assert torch.equal(got.isnan(), nan), f"{what}: NaN in other places"
@@ -64,9 +64,9 @@ def rope64(x, table, positions, sections, interleaved, inverse=False):
     return out, mag.nan_to_num(0.0, 0.0, 0.0)
 
 
-def linear64(x, w, bias=None, act=0, gate=None, residual=None):
+def linear64(x, w, bias=None, act=0, gate=None, residual=None, device="cpu"):
     """Returns (reference, slack)."""
-    f = lambda t: None if t is None else t.cpu().double()   # noqa: E731
+    f = lambda t: None if t is None else t.to(device).double()   # noqa: E731
     x, w, bias, gate, residual = map(f, (x, w, bias, gate, residual))
     M, K = x.shape
     z, mag = x @ w.t(), x.abs() @ w.abs().t()

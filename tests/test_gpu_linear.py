@@ -37,6 +37,45 @@ def test_product(shape, dtype):
     check(dvdq.linear(t["x"], t["w"], t["bias"], residual=t["residual"]), t["x"], t["w"], t["bias"], residual=t["residual"], what="residual")
 
 
+# (M, N, K, shape of tile, parts of K, whether workgroups take several tiles), every way an aligned product is taken
+WAYS = [(57652, 395, 312, 0, 1, True), (53282, 135, 272, 0, 1, False), (16728, 131, 4320, 0, 3, False), (2116, 7277, 784, 1, 1, True),
+        (17948, 142, 624, 1, 1, False), (5694, 134, 3400, 1, 4, False), (33862, 137, 72, 2, 1, True), (18670, 68, 80, 2, 1, False),
+        (70, 2705, 1432, 2, 6, False), (7212, 1093, 64, 3, 1, True), (8674, 67, 64, 3, 1, False), (70, 1407, 1296, 3, 6, False),
+        (34, 65, 72, 4, 1, False), (36, 67, 744, 4, 3, False)]
+TILES = [(256, 256, 1), (256, 128, 1), (128, 128, 2), (128, 64, 2), (64, 64, 4)]    # channels, tokens, workgroups per compute unit
+
+
+@pytest.mark.parametrize("way", WAYS)
+def test_every_way(way):
+    M, N, K, shape, parts, several = way
+    assert dvdq.bench_linear_choice(M, N, K) == shape + 16 * parts
+    bn, bm, per_cu = TILES[shape]
+    assert (-(-N // bn) * -(-M // bm) * parts > 256 * per_cu) == several
+    g = torch.Generator(device="cuda").manual_seed(7)
+    r = lambda *s, k=1.0: (k * torch.randn(s, generator=g, device="cuda")).to(torch.bfloat16)   # noqa: E731
+    x, w, bias, gate, res = r(M, K), r(N, K, k=K ** -0.5), r(N), r(2, N), r(M, N)
+    got = dvdq.linear(x, w, bias, 1, gate, res)
+    ref, slack = linear64(x, w, bias, 1, gate, res, device="cuda")
+    assert_close(got, ref, slack, str(way))
+    # and once more over the residual, with another gate and no bias
+    y = res.clone()
+    dvdq.linear(x, w, None, 2, gate[1], y, y=y)
+    ref, slack = linear64(x, w, None, 2, gate[1], res, device="cuda")
+    assert_close(y, ref, slack, str(way) + " in place")
+
+
+@pytest.mark.parametrize("shape,way", [((129, 257, 1157), 4 + 16 * 5 + 4096), ((9000, 3000, 203), 2 + 16 + 4096), ((300, 300, 33), 2 + 16 + 8192),
+                                       ((100, 1160, 1152), 2 + 16 * 4 + 8192), ((31, 96, 2048), 2 + 16 * 8 + 8192)])
+def test_every_way_of_unaligned_rows(shape, way):
+    M, N, K = shape
+    assert dvdq.bench_linear_choice(M, N, K, True) == way
+    g = torch.Generator(device="cuda").manual_seed(8)
+    x, w = (torch.randn((n, K + 3), generator=g, device="cuda").to(torch.float16)[:, 1:K + 1] for n in (M, N))
+    got = dvdq.linear(x, w)
+    ref, slack = linear64(x, w, device="cuda")
+    assert_close(got, ref, slack, str(shape))
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("shape", [(6, 200, 96), (90, 136, 256), (90, 133, 77), (720, 520, 640), (1026, 300, 1024)])

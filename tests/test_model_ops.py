@@ -69,6 +69,23 @@ def test_linear_argument_errors():
         assert linear(M=M, N=N, K=K, ldx=K, ldw=K, ldy=N, ws=None) == 1
 
 
+def test_linear_choice_is_the_same_every_time_and_sizes_the_workspace():
+    sizes = {0: (256, 256), 1: (256, 128), 2: (128, 128), 3: (128, 64), 4: (64, 64)}
+    for M, N, K in [(1, 64, 8), (16, 512, 4096), (17, 384, 1000), (512, 5120, 4096), (32760, 8960, 1536), (700, 300, 33), (3000, 500, 1157)]:
+        need, most = dvdq.linear_workspace_bytes(M, N, K), 0
+        for any_ in (False, True):
+            c = dvdq.bench_linear_choice(M, N, K, any_)
+            assert c == dvdq.bench_linear_choice(M, N, K, any_)
+            if c < 0:
+                continue
+            (bn, bm), parts = sizes[c & 15], (c >> 4) & 255
+            tiles = -(-N // bn) * -(-M // bm)
+            pad = -(-((M + N) * (-(-K // 64) * 64) * 2) // 256) * 256 if c & 4096 else 0
+            most = max(most, pad + (parts * tiles * bn * bm * 4 if parts > 1 else 0))
+        assert need == most, (M, N, K)
+    assert dvdq.bench_linear_choice(0, 1, 1) == -2
+
+
 def gn(x=FAKE, B=2, S=10, C=32, xb=320, xr=32, groups=4, w=None, b=None, eps=1e-5, act=0, dtype=0, y=FAKE + 65536, yb=320, yr=32, ws=FAKE, nws=1 << 40):
     return dvdq.lib().dvdq_group_norm(x, B, S, C, xb, xr, groups, w, b, eps, act, dtype, y, yb, yr, ws, nws, None)
 
