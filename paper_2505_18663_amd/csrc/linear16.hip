@@ -3,6 +3,11 @@
 //   y[m, n] = residual[m, n] + gate[m / (M / G), n] * act(sum_k x[m, k] w[n, k] + bias[n])
 //
 // Products on the matrix cores, sums and epilogue in fp32, one rounding to the tensors' type.
+//
+// Ways: linear_few (few tokens), linear_tiles (five shapes of tile, K in parts where there are few tiles: linear_join), rows that are no whole
+// 16-byte pieces copied first (linear_pad) or through registers (linear_any).  Against the library's product of the card's torch, which has no
+// epilogue: 32760 x 13824 x 5120 3190 to 3400 us and 2910, 32760 x 1536 x 8960 with GELU 800 to 840 and 660, 512 x 4096 x 5120 36 and 37, 64 x 5120 x 5120
+// 19 and 21, 1560 x 1536 x 1536 17 and 19, 2 x 1536 x 9216 8.3 and 19, 32760 x 1533 x 8960 810 and 890.
 #include <algorithm>
 
 #include "elem.h"
@@ -299,7 +304,7 @@ __global__ __launch_bounds__(256) void linear_join(LinearArgs a, int FM, int WN,
     if (m0 >= a.M || n0 >= a.N) return;
     v4f acc[4][1] = {};
     const float4 *p = a.parts + g * 256 + lane;
-#pragma unroll 2
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s, p += stride)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i][0] += __builtin_bit_cast(v4f, p[i * 64]);
