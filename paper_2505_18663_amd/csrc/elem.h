@@ -71,7 +71,11 @@ static __device__ __forceinline__ float sigmoid_times(float z, float t) {   // z
 template <int ACT>
 static __device__ __forceinline__ float activate(float z) {
     if constexpr (ACT == DVDQ_ACT_SILU) return sigmoid_times(z, z);
-    else if constexpr (ACT == DVDQ_ACT_GELU_TANH) return sigmoid_times(z, 1.5957691216057308f * (z + 0.044715f * z * z * z));
+    else if constexpr (ACT == DVDQ_ACT_GELU_TANH) {
+        // e^-2u = 2^(z (a + b z^2)), the constants multiplied out
+        const float t = z * fmaf(z * z, -0.10294324f, -2.3022082f);
+        return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t));
+    }
     else if constexpr (ACT == DVDQ_ACT_GELU) return 0.5f * z * (1.0f + erff(0.70710678118654752f * z));
     else return z;
 }
