@@ -6,7 +6,7 @@
 //
 // Ways: linear_few (few tokens), linear_tiles (five shapes of tile, K in parts where there are few tiles: linear_join), rows that are no whole
 // 16-byte pieces copied first (linear_pad) or through registers (linear_any).  Against the library's product of the card's torch, which has no
-// epilogue: 32760 x 13824 x 5120 3190 to 3400 us and 2910, 32760 x 1536 x 8960 with GELU 800 to 840 and 660, 512 x 4096 x 5120 36 and 37, 64 x 5120 x 5120
+// epilogue: 32760 x 13824 x 5120 gated 3270 to 3400 us and 2910, 32760 x 1536 x 8960 with GELU 745 to 790 and 660, 512 x 4096 x 5120 36 and 37, 64 x 5120 x 5120
 // 19 and 21, 1560 x 1536 x 1536 17 and 19, 2 x 1536 x 9216 8.3 and 19, 32760 x 1533 x 8960 810 and 890.
 #include <algorithm>
 

@@ -37,7 +37,7 @@ struct RopeKernelArgs {
 // goes through heads: the token's cosines and sines are read once and stay in registers.  Neighbouring threads hold neighbouring
 // pieces, so a wave reads and writes whole heads.  Up to six heads of a thread are in flight at a time.
 // Bound by memory: 118800 tokens x 48 heads of 128 in 16 bits, 2.9 GB in and out, in 490 us (6.0 TB/s; a copy on the same card 5.9),
-// 32760 x 24 in 70 (5.8).  What it took: cosines and sines in 16-byte loads where a piece lies within one axis (780 -> 637 us, one by
+// 32760 x 24 in 75 (5.4).  What it took: cosines and sines in 16-byte loads where a piece lies within one axis (780 -> 637 us, one by
 // one), streaming stores (-> 532), six heads a thread (-> 490).
 template <typename E, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeKernelArgs a) {
