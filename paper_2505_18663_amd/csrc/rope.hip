@@ -29,7 +29,7 @@ struct RopeKernelArgs {
     int n_axes;
     int bound[kMaxAxes - 1];                     // first pair of axes 1, 2, 3 (R/2 where there is none)
     int inverse;
-    int rot_units, units;                        // pieces per head that are rotated; those and the copied ones
+    int rot_units, units;                        // pieces per head that are rotated; those and the copied ones, as many as a workgroup takes
     int heads_at_once, tokens_per_block, heads_per_block;
 };
 
@@ -47,11 +47,12 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeKernelArgs a) {
     const int lt = (int)threadIdx.x / per_token, rem = (int)threadIdx.x - lt * per_token;
     const uint32_t token = blockIdx.x * (uint32_t)a.tokens_per_block + lt;
     if (lt >= a.tokens_per_block || token >= a.tokens) return;
-    const int hs = rem / a.units, u = rem - hs * a.units;
+    const int hs = rem / a.units, u = rem - hs * a.units + (int)blockIdx.z * kThreads;
     const uint32_t b = token / a.T, t = token - b * a.T;
     const int h_end = min(a.heads, ((int)blockIdx.y + 1) * a.heads_per_block);
     const int half = a.R / 2;
     const bool rotated = u < a.rot_units;
+    if (!rotated && a.R + (u - a.rot_units) * V >= a.D) return;   // (of a second workgroup's pieces)
 
     // where the piece lies in a head, and how many elements (of each half) of it there are
     const int j0 = u * PAIRS;                                  // first pair
@@ -182,17 +183,20 @@ int launch_rope(const dvdq_rope_heads *q, const dvdq_rope_heads *k, int64_t B, i
         const int per_unit = interleaved ? E::kVec : 2 * E::kVec;
         a.rot_units = (int)((R + per_unit - 1) / per_unit);
         // (in place, the part that is not rotated stays where it is)
-        a.units = a.rot_units + (in_place ? 0 : (int)((D - R + E::kVec - 1) / E::kVec));
+        const int units = a.rot_units + (in_place ? 0 : (int)((D - R + E::kVec - 1) / E::kVec));
+        // (both parts rounded up: 257 pieces of fp32 where a part of a head of 1023 or 1024 is rotated; the last one is a second workgroup's)
+        a.units = std::min(units, kThreads);
         // heads of a thread: as many as are in flight at a time, fewer where that leaves the chip with less than 512 threads per compute unit
         // (and, where a head is no whole lines, so that those that a token's threads write at once are 384 bytes at least: 46400 x 6 heads
         // of 72 16.5 us with three at once, 24 with one)
         const int head_bytes = (int)(D * sizeof(typename E::Raw)), at_once = head_bytes % 128 == 0 ? 1 : (383 + head_bytes) / head_bytes;
         int per_thread = std::clamp(a.heads / at_once, 1, kHeadsPerThread);
         while (per_thread > 1 && (int64_t)a.tokens * a.units * ((a.heads + per_thread - 1) / per_thread) < 256 * 512) --per_thread;
-        a.heads_at_once = std::min((a.heads + per_thread - 1) / per_thread, std::max(1, kThreads / a.units));
-        a.tokens_per_block = std::max(1, kThreads / (a.units * a.heads_at_once));
+        a.heads_at_once = std::min((a.heads + per_thread - 1) / per_thread, kThreads / a.units);
+        a.tokens_per_block = kThreads / (a.units * a.heads_at_once);
         a.heads_per_block = a.heads_at_once * per_thread;
-        const dim3 grid((a.tokens + a.tokens_per_block - 1) / a.tokens_per_block, (a.heads + a.heads_per_block - 1) / a.heads_per_block);
+        const dim3 grid((a.tokens + a.tokens_per_block - 1) / a.tokens_per_block, (a.heads + a.heads_per_block - 1) / a.heads_per_block,
+                        (units + kThreads - 1) / kThreads);
         // Streaming stores from 4 MB on, which is what an XCD's L2 holds: 2000 x 40 heads of 128 9.4 us, cached 13.6; below that the
         // outputs stay in the L2 for what reads them next (1022 x 16 heads of 80, 2.6 MB: 7.1 us, streaming 7.2).
         const bool stream_out = (int64_t)a.tokens * a.heads * D * (int64_t)sizeof(typename E::Raw) >= (4 << 20);
