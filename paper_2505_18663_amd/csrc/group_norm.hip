@@ -215,7 +215,8 @@ constexpr int kUnits = 8;
 template <typename E, int ACT, int V>
 __global__ __launch_bounds__(1024) void gn_whole(GnArgs a) {
     using Raw = typename E::Raw;
-    __shared__ float lds[2][16];
+    __shared__ double sums[16];
+    __shared__ float squares[16];
     const int g = blockIdx.x, b = blockIdx.y, threads = blockDim.x;
     const int per_row = a.cpg / V, total = (int)a.S * per_row;
     const Raw *x = static_cast<const Raw *>(a.x) + b * a.x_batch + g * a.cpg;
@@ -232,25 +233,32 @@ __global__ __launch_bounds__(1024) void gn_whole(GnArgs a) {
             if (c >= per_row) c -= per_row, ++row;
         }
     }
-    const float first = E::to_f32(x[0]), count = (float)((int)a.S * a.cpg);
-    float sum = 0.0f, m2 = 0.0f;
+    // a thread's own mean and squared deviations, joined by count: one value that is nothing like the others costs its own thread's few
+    // their last places, not the whole group (as differences to the group's first value would)
+    int pieces = 0;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) pieces += (int)threadIdx.x + i * threads < total;
+    const float first = E::to_f32(p[0].e[0]), n = (float)(pieces * V), count = (float)((int)a.S * a.cpg);
+    float own = 0.0f, m2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i)
-        if ((int)threadIdx.x + i * threads < total) {
+        if (i < pieces) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) sum += E::to_f32(p[i].e[j]) - first;
+            for (int j = 0; j < V; ++j) own += E::to_f32(p[i].e[j]) - first;
         }
-    const float mean = first + block_sum(sum, lds[0]) / count;
+    if (pieces) own = fmaf(own, __builtin_amdgcn_rcpf(n), first);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i)
-        if ((int)threadIdx.x + i * threads < total) {
+        if (i < pieces) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float d = E::to_f32(p[i].e[j]) - mean;
+                const float d = E::to_f32(p[i].e[j]) - own;
                 m2 = fmaf(d, d, m2);
             }
         }
-    const float rstd = (float)(1.0 / sqrt((double)block_sum(m2, lds[1]) / (double)count + (double)a.eps));
+    const float mean = (float)(block_sum((double)n * own, sums) / (double)count);   // (64 bits: exact where all are equal)
+    if (pieces) m2 = fmaf(n * (own - mean), own - mean, m2);
+    const float rstd = (float)(1.0 / sqrt((double)block_sum(m2, squares) / (double)count + (double)a.eps));
     int row = row0, c = c0;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
