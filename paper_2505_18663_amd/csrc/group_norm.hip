@@ -95,7 +95,12 @@ __global__ __launch_bounds__(1024) void gn_parts(GnArgs a) {
                         qb[j] = fmaf(d, d, qb[j]);
                     }
                 }
-            join<V>((float)i0, mean, m2, (float)nb, mb, qb);
+            if (i0 > 0) {
+                join<V>((float)i0, mean, m2, (float)nb, mb, qb);
+            } else {                                     // (there is nothing to join: a mean of 0 is no value's, and its difference may be beyond fp32 squared)
+#pragma unroll
+                for (int j = 0; j < V; ++j) mean[j] = mb[j], m2[j] = qb[j];
+            }
         }
         if constexpr (WHOLE) {
             float sum = 0.0f, m = 0.0f;
@@ -116,12 +121,13 @@ __global__ __launch_bounds__(1024) void gn_parts(GnArgs a) {
     __syncthreads();
     if constexpr (!WHOLE) {
         // per channel: mean and squared deviations over the slab, in the first two rows of lds
+        const int filled = min(a.rows_at_once, rows);   // rows of threads that have any
         for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
             const float first = lds[c];
             float sum = 0.0f, m2 = 0.0f;
-            for (int i = 1; i < a.rows_at_once; ++i) sum = fmaf((float)rows_of(i), lds[2 * i * width + c] - first, sum);
+            for (int i = 1; i < filled; ++i) sum = fmaf((float)rows_of(i), lds[2 * i * width + c] - first, sum);
             const float mean = first + sum / (float)rows;
-            for (int i = 0; i < a.rows_at_once; ++i) {
+            for (int i = 0; i < filled; ++i) {
                 const float d = lds[2 * i * width + c] - mean;
                 m2 += fmaf((float)rows_of(i), d * d, lds[(2 * i + 1) * width + c]);
             }
