@@ -560,10 +560,25 @@ def _need_view(t, dtype, shape, name, device=None):
     return t
 
 
-def _workspace(workspace, need, device):
+def _new(make, stream, kept=True):
+    """make(), a new tensor for work on `stream`, which belongs to that stream: what a call drops is reused in its order, not while its kernels
+    are still to run.  kept: the caller gets it, and may use and drop it on the current stream."""
+    if stream is None or _stream(stream) == _stream(None):
+        return make()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream))
+    current = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        t = make()
+    if kept:
+        t.record_stream(current)
+    return t
+
+
+def _workspace(workspace, need, device, stream):
     """The given workspace, or a new one where one is needed; and its size."""
     if workspace is None:
-        workspace = torch.empty((need,), dtype=torch.uint8, device=device) if need else None
+        workspace = _new(lambda: torch.empty((need,), dtype=torch.uint8, device=device), stream, kept=False) if need else None
     else:
         _need(workspace, torch.uint8, None, "workspace")
     return workspace, 0 if workspace is None else workspace.numel()
@@ -612,22 +627,23 @@ def rope_table(n_pos: int, freq, magnitude: float = 1.0, device="cuda", table=No
     pair (rope_frequencies, or a model's own), a sequence of numbers or an fp64 tensor on the GPU.  See dvdq_rope_table."""
     L = lib()
     if not isinstance(freq, torch.Tensor):
-        freq = torch.tensor(freq, dtype=torch.float64, device=device if table is None else table.device)
+        numbers, on = freq, device if table is None else table.device
+        freq = _new(lambda: torch.tensor(numbers, dtype=torch.float64, device=on), stream, kept=False)
     _need(freq, torch.float64, None, "freq")
     shape = (n_pos, freq.numel(), 2)
     if table is None:
-        table = torch.empty(shape, dtype=torch.float32, device=freq.device)
+        table = _new(lambda: torch.empty(shape, dtype=torch.float32, device=freq.device), stream)
     _need(table, torch.float32, shape, "table")
     _check(L.dvdq_rope_table(_ptr(freq), n_pos, freq.numel(), float(magnitude), _ptr(table), _stream(stream)), "dvdq_rope_table")
     return table
 
 
-def _rope_heads(x, out, D, name, dtype, lead):
+def _rope_heads(x, out, D, name, dtype, lead, stream):
     _need_view(x, dtype, None, name)
     if x.dim() != len(lead) + 2 or tuple(x.shape[:-2]) != lead or x.size(-1) != D:
         raise ValueError(f"{name}: expected shape {lead + ('heads', D)}, got {tuple(x.shape)}")
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _new(lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device), stream)
     else:
         _need_view(out, x.dtype, x.shape, name + "_out", x.device)
     st = [(0,) * (4 - t.dim()) + t.stride()[:-1] for t in (x, out)]
@@ -662,9 +678,9 @@ def rope(q, k, table, positions, sections=None, interleaved: bool = False, inver
         pos_batch = T * (axes[0] if axes else 1) if B > 1 else 0
     else:
         raise ValueError(f"positions: expected shape {(T,) + axes} or {(B, T) + axes}, got {tuple(positions.shape)}")
-    q_out, hq = _rope_heads(q, q_out, D, "q", q.dtype, lead)
+    q_out, hq = _rope_heads(q, q_out, D, "q", q.dtype, lead, stream)
     if k is not None:
-        k_out, hk = _rope_heads(k, k_out, D, "k", q.dtype, lead)
+        k_out, hk = _rope_heads(k, k_out, D, "k", q.dtype, lead, stream)
     for name, t in (("k", k), ("table", table), ("positions", positions)):
         if t is not None and t.device != q.device:
             raise ValueError(f"{name}: expected device {q.device}, got {t.device}")
@@ -708,10 +724,10 @@ def linear(x, w, bias=None, act: int = ACT_NONE, gate=None, residual=None, y=Non
     if residual is not None:
         _need_view(residual, x.dtype, (M, N), "residual", x.device)
     if y is None:
-        y = torch.empty((M, N), dtype=x.dtype, device=x.device)
+        y = _new(lambda: torch.empty((M, N), dtype=x.dtype, device=x.device), stream)
     else:
         _need_view(y, x.dtype, (M, N), "y", x.device)
-    workspace, n_ws = _workspace(workspace, L.dvdq_linear_workspace_bytes(M, N, K), x.device)
+    workspace, n_ws = _workspace(workspace, L.dvdq_linear_workspace_bytes(M, N, K), x.device, stream)
     _check(L.dvdq_linear(_ptr(x), x.stride(0), _ptr(w), w.stride(0), _ptr(bias), int(act), _ptr(gate), gate_rows,
                          gate.stride(0) if gate_rows > 1 else N, _ptr(residual), 0 if residual is None else residual.stride(0), M, N, K,
                          _DTYPES[x.dtype], _ptr(y), y.stride(0), _ptr(workspace), n_ws, _stream(stream)), "dvdq_linear")
@@ -754,14 +770,14 @@ def group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, act: i
         if t is not None:
             _need_view(t, x.dtype, (n_ch,), name, x.device)
     if y is None:
-        y = torch.empty_like(x)
+        y = _new(lambda: torch.empty_like(x), stream)
         if n_ch > 1 and y.stride(-1) != 1:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            y = _new(lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device), stream)
     else:
         _need_view(y, x.dtype, x.shape, "y", x.device)
     S, x_batch, x_row = _rows_of(x, "x")
     _, y_batch, y_row = _rows_of(y, "y")
-    workspace, n_ws = _workspace(workspace, L.dvdq_group_norm_workspace_bytes(B, S, n_ch, groups), x.device)
+    workspace, n_ws = _workspace(workspace, L.dvdq_group_norm_workspace_bytes(B, S, n_ch, groups), x.device, stream)
     _check(L.dvdq_group_norm(_ptr(x), B, S, n_ch, x_batch, x_row, int(groups), _ptr(weight), _ptr(bias), float(eps), int(act),
                              _DTYPES[x.dtype], _ptr(y), y_batch, y_row, _ptr(workspace), n_ws, _stream(stream)), "dvdq_group_norm")
     return y

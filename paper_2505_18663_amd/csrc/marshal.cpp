@@ -13,7 +13,10 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/StreamGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+
+#include <optional>
 
 #include "../../include/dvdq.h"
 
@@ -76,9 +79,14 @@ struct Args {
         ok = false;
         return nullptr;
     }
-    // the given view of that shape, or a new dense tensor of the type and on the device of `like`
-    at::Tensor output_like(int i, at::IntArrayRef shape, const at::Tensor &like) {
-        if (none(i)) return at::empty(shape, like.options());
+    // the given view of that shape, or a new dense tensor of the type and on the device of `like`: of the guard's stream, and in use on the
+    // caller's
+    at::Tensor output_like(int i, at::IntArrayRef shape, const at::Tensor &like, const std::optional<c10::StreamGuard> &guard) {
+        if (none(i)) {
+            at::Tensor t = at::empty(shape, like.options());
+            if (guard) t.record_stream(guard->original_stream());
+            return t;
+        }
         const at::Tensor *t = view(i, (int64_t)shape.size(), &like);
         if (!t || t->sizes() != shape) {
             ok = false;
@@ -117,16 +125,37 @@ struct Args {
         return (int)v;
     }
     // the handle of a torch.cuda.Stream, or of the current one for None; asked for last, when the tensors are known to be on a GPU
-    void *stream(int i) {
-        if (!ok) return nullptr;
+    void *stream(int i) { return ok ? handle(none(i) ? nullptr : a[i]) : nullptr; }
+    // The same; and where that is not the current stream, a guard under which new tensors are allocated for it: what this call drops may then
+    // be reused in that stream's order, not while its kernels are still to run.
+    void *stream(int i, std::optional<c10::StreamGuard> &guard) {
+        void *p = stream(i);
+        if (!ok || none(i) || p == handle(nullptr) || !ok) return p;
+        int64_t id[3] = {};   // (what a torch.cuda.Stream has; anything else goes through the Python function)
+        static const char *const names[3] = {"stream_id", "device_index", "device_type"};
+        for (int k = 0; k < 3 && ok; ++k) {
+            PyObject *v = PyObject_GetAttrString(a[i], names[k]);
+            ok = v && PyLong_Check(v);
+            if (ok) id[k] = PyLong_AsLongLong(v);
+            Py_XDECREF(v);
+        }
+        if (PyErr_Occurred()) {
+            PyErr_Clear();
+            ok = false;
+        }
+        if (ok) guard.emplace(c10::Stream::unpack3(id[0], (c10::DeviceIndex)id[1], (c10::DeviceType)id[2]));
+        return p;
+    }
+    // the handle of a stream object, or of the current stream
+    void *handle(PyObject *of) {
         PyObject *handle = nullptr;
-        if (none(i)) {
+        if (!of) {
             if (PyObject *device = PyObject_CallNoArgs(get_device)) {
                 handle = PyObject_CallOneArg(get_raw_stream, device);
                 Py_DECREF(device);
             }
         } else {
-            handle = PyObject_GetAttrString(a[i], "cuda_stream");
+            handle = PyObject_GetAttrString(of, "cuda_stream");
         }
         void *p = handle && PyLong_Check(handle) ? PyLong_AsVoidPtr(handle) : (ok = false, nullptr);
         Py_XDECREF(handle);
@@ -362,18 +391,19 @@ PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (k)
         for (int64_t i = 0; i < dim; ++i)
             if (i != dim - 2 && k->size(i) != q->size(i)) Py_RETURN_NONE;
+    std::optional<c10::StreamGuard> guard;
+    void *stream = a.stream(9, guard);
+    if (!a.ok) Py_RETURN_NONE;
     dvdq_rope_heads heads[2];
     at::Tensor out[2];
     for (int w = 0; w < (k ? 2 : 1); ++w) {
         const at::Tensor &x = w ? *k : *q;
-        out[w] = a.output_like(7 + w, x.sizes(), x);
+        out[w] = a.output_like(7 + w, x.sizes(), x, guard);
         if (!a.ok) Py_RETURN_NONE;
         heads[w] = {x.data_ptr(), out[w].data_ptr(), x.size(dim - 2),
                     {dim == 4 ? x.stride(0) : 0, x.stride(dim - 3), x.stride(dim - 2)},
                     {dim == 4 ? out[w].stride(0) : 0, out[w].stride(dim - 3), out[w].stride(dim - 2)}};
     }
-    void *stream = a.stream(9);
-    if (!a.ok) Py_RETURN_NONE;
     const int rc = unlocked([&] {
         return p_rope(&heads[0], k ? &heads[1] : nullptr, B, T, D, (const float *)table->data_ptr(), table->size(0), 2 * table->size(1),
                       (const int32_t *)pos->data_ptr(), p_dim == 2 && B > 1 ? T * axes : 0, axes, a.none(4) ? nullptr : sections,
@@ -398,9 +428,11 @@ PyObject *linear(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const int64_t M = x->size(0), K = x->size(1), N = w->size(0);
     if (w->size(1) != K || (bias && bias->size(0) != N) || (gate && gate->size(gate->dim() - 1) != N) || (res && (res->size(0) != M || res->size(1) != N)))
         Py_RETURN_NONE;
-    const at::Tensor y = a.output_like(6, {M, N}, *x);
+    std::optional<c10::StreamGuard> guard;
+    void *stream = a.stream(8, guard);
+    if (!a.ok) Py_RETURN_NONE;
+    const at::Tensor y = a.output_like(6, {M, N}, *x, guard);
     const at::Tensor ws = a.scratch(7, a.none(7) ? p_linear_workspace_bytes(M, N, K) : 0, *x);
-    void *stream = a.stream(8);
     if (!a.ok) Py_RETURN_NONE;
     const int64_t gate_rows = gate ? (gate->dim() == 1 ? 1 : gate->size(0)) : 0;
     const int rc = unlocked([&] {
@@ -423,9 +455,11 @@ PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (!a.ok || type < 0 || !PyFloat_CheckExact(args[4])) Py_RETURN_NONE;
     const int64_t B = x->size(0), S = x->size(1), C = x->size(2);
     if ((weight && weight->size(0) != C) || (bias && bias->size(0) != C)) Py_RETURN_NONE;
-    const at::Tensor y = a.output_like(6, x->sizes(), *x);
+    std::optional<c10::StreamGuard> guard;
+    void *stream = a.stream(8, guard);
+    if (!a.ok) Py_RETURN_NONE;
+    const at::Tensor y = a.output_like(6, x->sizes(), *x, guard);
     const at::Tensor ws = a.scratch(7, a.none(7) ? p_group_norm_workspace_bytes(B, S, C, groups) : 0, *x);
-    void *stream = a.stream(8);
     if (!a.ok) Py_RETURN_NONE;
     const float eps = (float)PyFloat_AS_DOUBLE(args[4]);
     const int rc = unlocked([&] {
