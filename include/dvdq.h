@@ -301,8 +301,9 @@ int dvdq_gbs_step(const void *f_t_bf16, const void *f_prev_bf16, int64_t n, floa
  *
  * Conventions as above, but for these: tensors are DVDQ_BF16, DVDQ_FP16 or (where said) DVDQ_FP32, all tensors of a call of one type;
  * they are views with strides, counted in elements, whose last dimension is dense; their addresses need only be those of an element
- * (DVDQ_ERR_ALIGN otherwise), workspaces and tables 16 bytes.  An output may be the input (or residual) itself, at the same address
- * with the same strides; other overlaps are the caller's to avoid.  Strides of an output may not be 0 over a dimension above 1, and an output
+ * (DVDQ_ERR_ALIGN otherwise), workspaces and tables 16 bytes.  An output may be the tensor that it is made of element by element, at the same
+ * address with the same strides: q and k of dvdq_rope, x of dvdq_group_norm, the residual of dvdq_linear (not its x, which all channels are made
+ * of).  Other overlaps are the caller's to avoid.  Strides of an output may not be 0 over a dimension above 1, and an output
  * that is an input may not have other strides (DVDQ_ERR_UNSUPPORTED).  A call over nothing (no batches, no tokens) does nothing and
  * returns DVDQ_OK.  NaN and infinities spread as in the formulas.
  */
@@ -359,7 +360,7 @@ int dvdq_rope_table(const double *freq, int64_t n_pos, int64_t half, double magn
  *   bias      in   [N] or NULL
  *   act            one of DVDQ_ACT_*
  *   gate      in   [gate_rows, N], rows ldg apart, or NULL; gate_rows divides M: each row is for M / gate_rows consecutive tokens
- *   residual  in   [M, N], rows ldr apart, or NULL; may be y
+ *   residual  in   [M, N], rows ldr apart, or NULL; may be y (x and w may not, nor bias and gate unless each is read once only: DVDQ_ERR_UNSUPPORTED)
  *   y         out  [M, N], rows ldy apart
  *   workspace      device, 16-byte aligned, at least dvdq_linear_workspace_bytes(M, N, K) (which may be 0: then NULL will do).
  *                  Scratch: calls that may run at the same time need one each

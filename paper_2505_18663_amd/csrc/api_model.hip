@@ -83,6 +83,8 @@ int dvdq_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const vo
     if (M > kMaxTokens || N > kMaxChannels || K > kMaxChannels || act < DVDQ_ACT_NONE || act > DVDQ_ACT_GELU || (dtype != DVDQ_BF16 && dtype != DVDQ_FP16) ||
         (residual == y && M > 1 && ldr != ldy) || (M > 1 && (ldy > kMaxPitch || (residual && ldr > kMaxPitch))))
         return DVDQ_ERR_UNSUPPORTED;
+    // operands of which other outputs still need what an output would overwrite
+    if (y == x || y == w || (y == bias && M > 1) || (y == gate && (gate_rows != M || (M > 1 && ldg != ldy)))) return DVDQ_ERR_UNSUPPORTED;
     for (const void *p : {x, w, bias, gate, residual, static_cast<const void *>(y)})
         if (!aligned_to(p, 2)) return DVDQ_ERR_ALIGN;
     const size_t need = dvdq::linear_workspace_bytes(M, N, K);
