@@ -755,7 +755,8 @@ def _rows_of(t, name):
 def group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, act: int = ACT_NONE, y=None, workspace=None, stream=None):
     """y = act(group norm of x), channels last: x [B, ..., C] (bf16, fp16 or fp32; a channels-last module's tensor as
     x.movedim(1, -1)), statistics over the dimensions in between and each of `groups` runs of channels; weight and bias [C] of the same
-    type; act ACT_NONE or ACT_SILU; y may be x.  Returns y.  See dvdq_group_norm."""
+    type; act ACT_NONE or ACT_SILU; y may be x, and is a new tensor that lies in memory as x does if not given.  Returns y.  See
+    dvdq_group_norm."""
     L = lib()
     r = _marshal.group_norm(x, groups, weight, bias, eps, act, y, workspace, stream)
     if r is not None:

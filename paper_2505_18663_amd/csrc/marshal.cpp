@@ -458,7 +458,15 @@ PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
     std::optional<c10::StreamGuard> guard;
     void *stream = a.stream(8, guard);
     if (!a.ok) Py_RETURN_NONE;
-    const at::Tensor y = a.output_like(6, x->sizes(), *x, guard);
+    // (a new output lies in memory as x does, where that leaves its channels dense)
+    at::Tensor y;
+    if (a.none(6)) {
+        y = at::empty_like(*x);
+        if (C > 1 && y.stride(2) != 1) y = at::empty(x->sizes(), x->options());
+        if (guard) y.record_stream(guard->original_stream());
+    } else {
+        y = a.output_like(6, x->sizes(), *x, guard);
+    }
     const at::Tensor ws = a.scratch(7, a.none(7) ? p_group_norm_workspace_bytes(B, S, C, groups) : 0, *x);
     if (!a.ok) Py_RETURN_NONE;
     const float eps = (float)PyFloat_AS_DOUBLE(args[4]);
