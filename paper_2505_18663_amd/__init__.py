@@ -581,6 +581,8 @@ def _workspace(workspace, need, device, stream):
         workspace = _new(lambda: torch.empty((need,), dtype=torch.uint8, device=device), stream, kept=False) if need else None
     else:
         _need(workspace, torch.uint8, None, "workspace")
+        if workspace.device != device:
+            raise ValueError(f"workspace: expected device {device}, got {workspace.device}")
     return workspace, 0 if workspace is None else workspace.numel()
 
 

@@ -94,11 +94,12 @@ struct Args {
         }
         return *t;
     }
-    // scratch: the given bytes, or as many as are needed on the device of `like`
+    // scratch on the device of `like`: the given bytes, or as many as are needed
     at::Tensor scratch(int i, size_t need, const at::Tensor &like) {
         if (!none(i)) {
             const at::Tensor *t = tensor(i, at::kByte);
-            return t ? *t : at::Tensor();
+            ok = t && t->device() == like.device();
+            return ok ? *t : at::Tensor();
         }
         return need ? at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(like.device())) : at::Tensor();
     }
