@@ -379,7 +379,7 @@ size_t dvdq_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
  *     y[b, s, c] = act((x[b, s, c] - mean[b, g]) / sqrt(var[b, g] + eps) * weight[c] + bias[c]),   g = c / (C / groups)
  *
  * with mean and biased variance over the S rows (all positions of a frame or clip) and C / groups channels of the group; statistics
- * and arithmetic in fp32 or more, rounded once.
+ * and arithmetic in fp32 or more, rounded once (deviations beyond 1.8e19, whose squares fp32 does not hold, make the variance infinite).
  *   x, y           [B, S, C]: batches x_batch, rows x_row elements apart; any of the three types; y may be x
  *   weight, bias   [C] or NULL, of the same type
  *   act            DVDQ_ACT_NONE or DVDQ_ACT_SILU (DVDQ_ERR_UNSUPPORTED otherwise)

@@ -6,8 +6,8 @@
 //
 // Ways: linear_few (few tokens), linear_tiles (five shapes of tile, K in parts where there are few tiles: linear_join), rows that are no whole
 // 16-byte pieces copied first (linear_pad) or through registers (linear_any).  Against the library's product of the card's torch, which has no
-// epilogue: 32760 x 13824 x 5120 gated 3270 to 3400 us and 2910, 32760 x 1536 x 8960 with GELU 745 to 790 and 660, 512 x 4096 x 5120 36 and 37, 64 x 5120 x 5120
-// 19 and 21, 1560 x 1536 x 1536 17 and 19, 2 x 1536 x 9216 8.3 and 19, 32760 x 1533 x 8960 810 and 890.
+// epilogue, weights out of the caches: 32760 x 13824 x 5120 with a residual 3260 to 3400 us and 2920, 32760 x 1536 x 8960 with tanh GELU 750 to 790 and 650 to 690,
+// 512 x 4096 x 5120 35 and 36, 64 x 5120 x 5120 20 and 22, 1560 x 1536 x 1536 17 and 20, 2 x 1536 x 9216 9.1 and 20, 32760 x 1533 x 8960 740 to 780 and 890.
 #include <algorithm>
 
 #include "elem.h"
@@ -38,7 +38,7 @@ struct LinearArgs {
     float4 *parts;                     // sums of parts of K, in the order of the accumulators (kPart)
     int splits, slices;                // parts of K; slices of 64 of a part
     // Outputs past the caches, where they are larger than an XCD's L2 and the 64 bytes that the lanes of a token write are sectors of their own
-    // (rows and address multiples of 64 bytes): 32760 x 1536 x 8960 with GELU 813 -> 753 us, 32760 x 1536 x 4608 399 -> 368, 118800 x 1536 x 1536 515 -> 503.
+    // (rows and address multiples of 64 bytes): 32760 x 1536 x 8960 with tanh GELU 823 -> 775 us, 32760 x 1536 x 4608 395 -> 364, 118800 x 1536 x 1536 513 -> 510.
     bool streaming;
 };
 constexpr int kPart = 4;               // in the place of an activation: leave the sums of a part of K for linear_join
@@ -202,9 +202,9 @@ __global__ __launch_bounds__(256, 2) void linear_any(LinearArgs a) {
 // A workgroup has 16 channels, its waves parts of K: a lane reads 32 bytes of a channel (the four lanes of a channel a whole line) and the same part of its
 // token, two matrix instructions' worth, twice over before the first product; the waves' sums meet in LDS in their order.
 // (The instruction's order of K does not matter as long as it is the same on both sides.)
-// 2 x 1536 x 9216, 28 MB of weights: 8.9 us with 8 waves, 12.8 with 16, 9.9 with 4; as tiles 14.0.  1 x 1536 x 4608 6.8 and 11.9, 16 x 1536 x 13824
-// 14.9 and 17.9, 2 x 5120 x 30720 57 and 66.  Few channels leave compute units idle and long rows their waves with too little in flight:
-// 8 x 13824 x 128 22 and 14, 16 x 5120 x 5120 23 and 19, 2 x 13824 x 5120 36 and 36; these are tiles.
+// 2 x 1536 x 9216, 28 MB of weights: 9.1 us with 8 waves (8.3 where the caches hold the weights), 9.5 with 16, 9.6 with 4; as tiles 14.1.
+// 1 x 1536 x 4608 6.5 and 11.9, 16 x 1536 x 13824 15.0 and 18.2, 2 x 5120 x 30720 57 and 67.  Few channels leave compute units idle and long rows their
+// waves with too little in flight: 8 x 13824 x 128 22 and 15, 16 x 5120 x 5120 23 and 19, 2 x 13824 x 5120 36 and 36; these are tiles.
 constexpr int kFewWaves = 8;
 inline bool few_tokens(int64_t M, int64_t N, int64_t K) { return M <= 16 && (K <= 4096 || N >= 16384); }
 template <typename E, int ACT>
@@ -329,7 +329,7 @@ __device__ uint4 zero_piece;   // what the pieces past K of the last slice are r
 // Tiles of 64 WN channels x 16 FM WM tokens, WN x WM waves of 64 channels x 16 FM tokens each; slices of 64 elements of K.
 // Weights have three slices in LDS, tokens two: while a slice is multiplied, the next is there, the weights of the one after it
 // come in, and its tokens follow as soon as those of the present slice have been read.  (What bounds the loop on a full chip is the way from
-// the L2s into LDS, 55 to 65 GB/s per compute unit where 32 of them share panels; it must not run dry.)
+// the L2s into LDS, 54 to 69 GB/s per compute unit where 32 of them share panels; it must not run dry.)
 // A slice is worked off in phases of 16 matrix instructions (or fewer), and a phase begins by requesting the fragments of the next one.
 // Before the last phase of a slice, whose fragments are then in registers, stands the slice's one barrier: behind it the next slice is
 // in LDS for every wave, and this one's place is free.
@@ -551,7 +551,7 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
         }
     }
     // Rows that are no whole pieces: copied into ones that are, where that takes less than what linear_any loses (its registers on the way to
-    // LDS cost it 1.4 to 1.9 times the time of 128 x 128 tiles: 32760 x 1533 x 8960 1655 us, copied 812).
+    // LDS cost it 1.4 to 1.9 times the time of 128 x 128 tiles: 32760 x 1533 x 8960 1388 us, copied 780).
     if (any && K % 8 != 0) {
         const int64_t pitch = (K + 63) / 64 * 64;
         LinearPlan p = linear_plan(M, N, pitch, false);
