@@ -245,7 +245,8 @@ __global__ __launch_bounds__(1024) void gn_whole(GnArgs a) {
     int pieces = 0;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) pieces += (int)threadIdx.x + i * threads < total;
-    const float first = E::to_f32(p[0].e[0]), n = (float)(pieces * V), count = (float)((int)a.S * a.cpg);
+    const float first = E::to_f32(p[0].e[0]), n = (float)(pieces * V);
+    const double share = 1.0 / (double)((int)a.S * a.cpg);   // of a value (done by the time the values are there)
     float own = 0.0f, m2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i)
@@ -263,9 +264,9 @@ __global__ __launch_bounds__(1024) void gn_whole(GnArgs a) {
                 m2 = fmaf(d, d, m2);
             }
         }
-    const float mean = (float)(block_sum((double)n * own, sums) / (double)count);   // (64 bits: exact where all are equal)
+    const float mean = (float)(block_sum((double)n * own, sums) * share);   // (64 bits: exact where all are equal)
     if (pieces) m2 = fmaf(n * (own - mean), own - mean, m2);
-    const float rstd = (float)(1.0 / sqrt((double)block_sum(m2, squares) / (double)count + (double)a.eps));
+    const float rstd = (float)rsqrt((double)block_sum(m2, squares) * share + (double)a.eps);
     int row = row0, c = c0;
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
