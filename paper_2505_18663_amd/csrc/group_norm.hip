@@ -217,7 +217,7 @@ __global__ __launch_bounds__(256) void gn_join(GnArgs a) {
 }
 
 // A whole group in a workgroup's registers: read once, written once, one launch.  V: elements of a piece of a row of the group.  Taken
-// where a group is at most 8192 pieces: 1560 x 512 in 32 groups, 3.2 MB, 9.0 us a call, most of it the launch (three launches 19).
+// where a group is at most 8192 pieces: 1560 x 512 in 32 groups, 3.2 MB, 8.9 us a call, most of it the launch (three launches 19).
 constexpr int kUnits = 8;
 template <typename E, int ACT, int V>
 __global__ __launch_bounds__(1024) void gn_whole(GnArgs a) {

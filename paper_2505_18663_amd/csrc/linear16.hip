@@ -6,8 +6,9 @@
 //
 // Ways: linear_few (few tokens), linear_tiles (five shapes of tile, K in parts where there are few tiles: linear_join), rows that are no whole
 // 16-byte pieces copied first (linear_pad) or through registers (linear_any).  Against the library's product of the card's torch, which has no
-// epilogue, weights out of the caches: 32760 x 13824 x 5120 with a residual 3260 to 3400 us and 2920, 32760 x 1536 x 8960 with tanh GELU 750 to 790 and 650 to 690,
-// 512 x 4096 x 5120 35 and 36, 64 x 5120 x 5120 20 and 22, 1560 x 1536 x 1536 17 and 20, 2 x 1536 x 9216 9.1 and 20, 32760 x 1533 x 8960 740 to 780 and 890.
+// epilogue, weights out of the caches (a fast card and a slow one): 32760 x 13824 x 5120 with a residual 3260 to 3520 us and 2920 to 3120, 32760 x 1536 x 8960
+// with tanh GELU 755 to 820 and 660 to 750, 512 x 4096 x 5120 35 to 37 and 36 to 38, 64 x 5120 x 5120 20 and 22, 1560 x 1536 x 1536 17 and 20, 2 x 1536 x 9216
+// 9.1 and 20, 32760 x 1533 x 8960 740 to 780 and 890 to 910.
 #include <algorithm>
 
 #include "elem.h"
