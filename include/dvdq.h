@@ -391,6 +391,81 @@ int dvdq_group_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_ba
                     void *workspace, size_t workspace_bytes, void *hip_stream);
 size_t dvdq_group_norm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t groups);
 
+/* ------------------------------------------------------------------------------------------------
+ * Layers whose weights and activations have 8 bits each, with a scale per token and per channel, and the norm in front of them.
+ * Conventions as in the part above.  Codes are int8 in [-127, 127], rows of any pitch at any address; a row's scale is what one step stands for.
+ * They are those of dvdq_rotate_quant too: its codes of 8 bits (DVDQ_CODES_INT8) go into dvdq_linear8, and the codes made here, dense rows, into
+ * dvdq_w4ax_gemm (act_bits = 8).
+ *
+ * Codes are whole numbers next to 127 z / max|z|, ties to the even one, max over the row: those of the real numbers z that the formulas give
+ * (activations and products in more than fp32 where a value is next to the border between two codes).  A row of zeros has scale 0.  A
+ * row that holds a NaN or an infinity (z beyond fp32 counts as one) has codes 0 and scale NaN, so that its products are NaN.
+ */
+
+/*
+ * Root-mean-square norm, with the residual's addition in front:
+ *
+ *     h[b, s, :] = x[b, s, :] + residual[b, s, :]        rounded to the tensors' type; x itself without a residual
+ *     y[b, s, c] = h[b, s, c] * weight[c] / sqrt(mean_c h[b, s, c]^2 + eps)
+ *
+ * with the statistic in fp32 (squares beyond fp32 make it infinite), one rounding.
+ *   x         in   [B, S, C]: batches x_batch, rows x_row elements apart; any of the three types; any strides (the heads of a projection's
+ *                  output are a batch's rows)
+ *   residual  in   the same with its own strides, or NULL
+ *   h         out  where the sum goes, which may be x or the residual; NULL without a residual (DVDQ_ERR_SHAPE otherwise)
+ *   weight    in   [C] of the same type, or NULL
+ *   y         out  may be x or the residual, where h is not there
+ * C at most 2^22, B S below 2^31 (DVDQ_ERR_UNSUPPORTED); eps >= 0 (DVDQ_ERR_SHAPE).
+ */
+int dvdq_rms_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_batch, int64_t x_row, const void *residual, int64_t r_batch,
+                  int64_t r_row, void *h, int64_t h_batch, int64_t h_row, const void *weight, float eps, int dtype, void *y, int64_t y_batch,
+                  int64_t y_row, void *hip_stream);
+
+/*
+ * The same with its output in 8 bits, y = x_scale codes, without a rounding to the tensors' type in between:
+ *   codes        out  int8 [B, S, C], batches c_batch, rows c_row apart
+ *   x_scale      out  fp32 [B, S], dense
+ *   code_rowsum  out  int32 [B, S], dense, or NULL: the sums of the rows' codes, which dvdq_w4ax_gemm needs for weights with zero-points
+ */
+int dvdq_rms_norm_quant(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_batch, int64_t x_row, const void *residual, int64_t r_batch,
+                        int64_t r_row, void *h, int64_t h_batch, int64_t h_row, const void *weight, float eps, int dtype, int8_t *codes,
+                        int64_t c_batch, int64_t c_row, float *x_scale, int32_t *code_rowsum, void *hip_stream);
+
+/*
+ * Rows to 8 bits: activations that no norm precedes, with what stands in front of the next product, and weights (a row per channel).
+ *
+ *     act(x[m, c]) * up[m, c] = x_scale[m] codes[m, c]
+ *
+ *   x            in   [M, C], rows ldx apart; any of the three types
+ *   up           in   [M, C] of the same type, rows ldu apart, or NULL (1).  A gated feed-forward's two halves are views of one product's output
+ *   act               one of DVDQ_ACT_*
+ *   codes        out  int8 [M, C], rows ldc apart
+ *   x_scale      out  fp32 [M]
+ *   code_rowsum  out  int32 [M] or NULL
+ * C at most 2^22, M below 2^31 (DVDQ_ERR_UNSUPPORTED); ldc >= C (DVDQ_ERR_SHAPE).
+ */
+int dvdq_quant8(const void *x, int64_t ldx, const void *up, int64_t ldu, int act, int64_t M, int64_t C, int dtype, int8_t *codes, int64_t ldc,
+                float *x_scale, int32_t *code_rowsum, void *hip_stream);
+
+/*
+ * Matrix product of 8-bit codes and weights with the epilogue of dvdq_linear:
+ *
+ *     y[m, n] = residual[m, n] + gate[m / (M / gate_rows), n] * act(x_scale[m] w_scale[n] sum_k codes[m, k] w[n, k] + bias[n])
+ *
+ * Sums are exact (int32); scales and the rest in fp32, one rounding to `dtype`, which may be any of the three and is that of bias, gate, residual and y.
+ *   codes     in   int8 [M, K], rows ldc apart; any values
+ *   x_scale   in   fp32 [M]
+ *   w         in   int8 [N, K], rows ldw apart; any values
+ *   w_scale   in   fp32 [N]
+ * The others, and the workspace (dvdq_linear8_workspace_bytes), as for dvdq_linear.  Rows that begin at multiples of 16 bytes are read
+ * where they lie; others are copied first, or read through registers.
+ * K at most 131071 (no sum of products can leave int32), the rest as for dvdq_linear (DVDQ_ERR_UNSUPPORTED).
+ */
+int dvdq_linear8(const int8_t *codes, int64_t ldc, const float *x_scale, const int8_t *w, int64_t ldw, const float *w_scale, const void *bias, int act,
+                 const void *gate, int64_t gate_rows, int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype,
+                 void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *hip_stream);
+size_t dvdq_linear8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+
 const char *dvdq_status_string(int status);
 int dvdq_version(void);
 

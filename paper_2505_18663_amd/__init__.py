@@ -26,6 +26,7 @@ __all__ = [
     "rotate_quant", "rotate_quant_blockwise", "w4ax_gemm", "qlinear", "qlinear_static", "static_workspace_bytes", "qlinear_workspace_bytes", "qlinear_scale_offset", "qlinear_rowsum_offset", "workspace_rowsum",
     "w4_prepack", "w4_native_bytes", "w4_prepack_fp6", "w4_native_fp6_bytes", "codes_bytes", "bgr_quantize", "GbsController",
     "rope_frequencies", "rope_table", "rope", "linear", "linear_workspace_bytes", "group_norm", "group_norm_workspace_bytes",
+    "rms_norm", "rms_norm_quant", "quant8", "linear8", "linear8_workspace_bytes",
     "ACT_NONE", "ACT_SILU", "ACT_GELU_TANH", "ACT_GELU", "bench_copy", "bench_mfma_i8", "bench_mfma_fp6", "bench_set_gemm_variant", "bench_set_gemm_schedule", "bench_fill_tile_counters", "bench_set_gemm_grid_limit", "release_stream",
     "W_CANONICAL", "W_NATIVE", "W_NATIVE_FP6", "CODES_INT8", "CODES_PACKED4", "CODES_FP6", "BGR_LISTING", "BGR_BEST_OF_ALL", "EXPORTED_SYMBOLS",
 ]
@@ -40,6 +41,7 @@ EXPORTED_SYMBOLS = (
     "dvdq_qlinear_scale_offset", "dvdq_qlinear_rowsum_offset", "dvdq_qlinear_static", "dvdq_static_workspace_bytes", "dvdq_w4_prepack", "dvdq_w4_native_bytes", "dvdq_w4_prepack_fp6",
     "dvdq_w4_native_fp6_bytes", "dvdq_codes_bytes", "dvdq_status_string",
     "dvdq_version", "dvdq_rope", "dvdq_rope_table", "dvdq_linear", "dvdq_linear_workspace_bytes", "dvdq_bench_linear_choice", "dvdq_group_norm", "dvdq_group_norm_workspace_bytes",
+    "dvdq_rms_norm", "dvdq_rms_norm_quant", "dvdq_quant8", "dvdq_linear8", "dvdq_linear8_workspace_bytes",
     "dvdq_gbs_workspace_bytes", "dvdq_gbs_reset", "dvdq_gbs_step", "dvdq_bgr_quantize", "dvdq_bench_copy", "dvdq_bench_mfma_i8", "dvdq_bench_mfma_fp6", "dvdq_bench_set_gemm_variant", "dvdq_bench_set_gemm_schedule", "dvdq_bench_fill_tile_counters", "dvdq_bench_set_gemm_grid_limit", "dvdq_bench_set_gbs_wait", "dvdq_bench_gemm_choice", "dvdq_bench_narrow_tiles", "dvdq_bench_quantizer_waves", "dvdq_bench_qlinear_choice", "dvdq_bench_bgr_choice", "dvdq_release_stream",
 )
 
@@ -71,6 +73,7 @@ class _Handback:
     def _hand_back(*args):
         return None
     rotate_quant = rotate_quant_blockwise = w4ax_gemm = qlinear = gbs_reset = gbs_step = rope = linear = group_norm = _hand_back
+    rms_norm = rms_norm_quant = quant8 = linear8 = _hand_back
 
 
 def _load_marshal(L):
@@ -84,7 +87,8 @@ def _load_marshal(L):
     native.bind(torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream, *(C.cast(getattr(L, f), C.c_void_p).value for f in (
         "dvdq_rotate_quant", "dvdq_rotate_quant_blockwise", "dvdq_w4ax_gemm", "dvdq_qlinear", "dvdq_gbs_reset", "dvdq_gbs_step",
         "dvdq_codes_bytes", "dvdq_qlinear_workspace_bytes", "dvdq_w4_native_bytes", "dvdq_w4_native_fp6_bytes",
-        "dvdq_rope", "dvdq_linear", "dvdq_linear_workspace_bytes", "dvdq_group_norm", "dvdq_group_norm_workspace_bytes")))
+        "dvdq_rope", "dvdq_linear", "dvdq_linear_workspace_bytes", "dvdq_group_norm", "dvdq_group_norm_workspace_bytes",
+        "dvdq_rms_norm", "dvdq_rms_norm_quant", "dvdq_quant8", "dvdq_linear8", "dvdq_linear8_workspace_bytes")))
     return native
 
 
@@ -147,6 +151,17 @@ def lib() -> C.CDLL:
     L.dvdq_group_norm.restype = i32
     L.dvdq_group_norm_workspace_bytes.argtypes = [i64, i64, i64, i64]
     L.dvdq_group_norm_workspace_bytes.restype = sz
+    rows = [vp, i64, i64, i64, i64, i64, vp, i64, i64, vp, i64, i64, vp, C.c_float, i32]   # x .. dtype
+    L.dvdq_rms_norm.argtypes = [*rows, vp, i64, i64, vp]
+    L.dvdq_rms_norm.restype = i32
+    L.dvdq_rms_norm_quant.argtypes = [*rows, vp, i64, i64, vp, vp, vp]
+    L.dvdq_rms_norm_quant.restype = i32
+    L.dvdq_quant8.argtypes = [vp, i64, vp, i64, i32, i64, i64, i32, vp, i64, vp, vp, vp]
+    L.dvdq_quant8.restype = i32
+    L.dvdq_linear8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i32, vp, i64, i64, vp, i64, i64, i64, i64, i32, vp, i64, vp, sz, vp]
+    L.dvdq_linear8.restype = i32
+    L.dvdq_linear8_workspace_bytes.argtypes = [i64, i64, i64]
+    L.dvdq_linear8_workspace_bytes.restype = sz
     L.dvdq_bench_copy.argtypes = [vp, vp, sz, vp]
     L.dvdq_bench_mfma_i8.argtypes = [i32, i32, vp, C.POINTER(C.c_double), vp]
     L.dvdq_bench_mfma_fp6.argtypes = [i32, i32, vp, C.POINTER(C.c_double), vp]
@@ -783,6 +798,167 @@ def group_norm(x, groups: int, weight=None, bias=None, eps: float = 1e-5, act: i
     workspace, n_ws = _workspace(workspace, L.dvdq_group_norm_workspace_bytes(B, S, n_ch, groups), x.device, stream)
     _check(L.dvdq_group_norm(_ptr(x), B, S, n_ch, x_batch, x_row, int(groups), _ptr(weight), _ptr(bias), float(eps), int(act),
                              _DTYPES[x.dtype], _ptr(y), y_batch, y_row, _ptr(workspace), n_ws, _stream(stream)), "dvdq_group_norm")
+    return y
+
+
+# ------------------------------------------------------------------ layers in 8 bits
+def _on_current_device(t, name):
+    """A launch goes to the current device, and must find its tensors there."""
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name}: lies on {t.device}, which is not the current device")
+
+
+def _dense(t, dtype, shape, name, device):
+    _need(t, dtype, shape, name)
+    if t.device != device:
+        raise ValueError(f"{name}: expected device {device}, got {t.device}")
+    return t
+
+
+def _norm_rows(x, weight, residual, h, stream):
+    """Checks of the norm's inputs; (h, the C arguments from x to weight)."""
+    _need_view(x, None, None, "x")
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"x: expected bfloat16, float16 or float32, got {x.dtype}")
+    if x.dim() < 2:
+        raise ValueError("x: expected shape [..., C] of two dimensions or more")
+    _on_current_device(x, "x")
+    if weight is not None:
+        _need_view(weight, x.dtype, (x.size(-1),), "weight", x.device)
+    if residual is None:
+        if h is not None:
+            raise ValueError("h: takes the sum of x and a residual, and there is none")
+        r_rows = h_rows = (None, 0, 0)
+    else:
+        _need_view(residual, x.dtype, x.shape, "residual", x.device)
+        if h is None:
+            h = _new(lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device), stream)
+        else:
+            _need_view(h, x.dtype, x.shape, "h", x.device)
+        r_rows, h_rows = ((_ptr(t), *_rows_of(t, name)[1:]) for t, name in ((residual, "residual"), (h, "h")))
+    S, x_batch, x_row = _rows_of(x, "x")
+    return h, (_ptr(x), x.size(0), S, x.size(-1), x_batch, x_row, *r_rows, *h_rows, _ptr(weight))
+
+
+def _row_codes(x, codes, x_scale, want_rowsum, code_rowsum, stream):
+    """Outputs of a call that leaves x's rows in 8 bits: (codes, x_scale, code_rowsum or None)."""
+    if codes is None:
+        codes = _new(lambda: torch.empty(x.shape, dtype=torch.int8, device=x.device), stream)
+    else:
+        _need_view(codes, torch.int8, x.shape, "codes", x.device)
+    lead = tuple(x.shape[:-1])
+    if x_scale is None:
+        x_scale = _new(lambda: torch.empty(lead, dtype=torch.float32, device=x.device), stream)
+    else:
+        _dense(x_scale, torch.float32, lead, "x_scale", x.device)
+    if code_rowsum is not None:
+        _dense(code_rowsum, torch.int32, lead, "code_rowsum", x.device)
+    elif want_rowsum:
+        code_rowsum = _new(lambda: torch.empty(lead, dtype=torch.int32, device=x.device), stream)
+    return codes, x_scale, code_rowsum
+
+
+def rms_norm(x, weight=None, residual=None, eps: float = 1e-6, h=None, y=None, stream=None):
+    """y = h * weight / sqrt(mean(h^2) + eps) over the last dimension, h = x + residual rounded to x's type (x itself without a
+    residual).  x: [..., C] of two dimensions or more, bf16, fp16 or fp32, any strides with dense channels (the dimensions between the first and
+    the last must be those of one sequence of rows: a projection's heads as [tokens, heads, D]); weight [C], residual like x.  h: where the sum
+    goes, e.g. the residual itself; y may be x.  Both are new dense tensors if not given.  Returns y, with a residual (y, h).  See dvdq_rms_norm."""
+    L = lib()
+    r = _marshal.rms_norm(x, weight, residual, eps, h, y, stream)
+    if r is not None:
+        return _native(r, "dvdq_rms_norm")
+    h, args = _norm_rows(x, weight, residual, h, stream)
+    if y is None:
+        y = _new(lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device), stream)
+    else:
+        _need_view(y, x.dtype, x.shape, "y", x.device)
+    _check(L.dvdq_rms_norm(*args, float(eps), _DTYPES[x.dtype], _ptr(y), *_rows_of(y, "y")[1:], _stream(stream)), "dvdq_rms_norm")
+    return y if residual is None else (y, h)
+
+
+def rms_norm_quant(x, weight=None, residual=None, eps: float = 1e-6, h=None, codes=None, x_scale=None, want_rowsum: bool = False,
+                   code_rowsum=None, stream=None):
+    """The norm with its output in 8 bits, for linear8 (or w4ax_gemm with act_bits=8): (codes int8 like x, x_scale fp32 [...][, code_rowsum
+    int32 [...]][, h]).  code_rowsum comes with want_rowsum (or where it is given), h with a residual.  See dvdq_rms_norm_quant."""
+    L = lib()
+    r = _marshal.rms_norm_quant(x, weight, residual, eps, h, codes, x_scale, want_rowsum, code_rowsum, stream)
+    if r is not None:
+        return _native(r, "dvdq_rms_norm_quant")
+    h, args = _norm_rows(x, weight, residual, h, stream)
+    codes, x_scale, code_rowsum = _row_codes(x, codes, x_scale, want_rowsum, code_rowsum, stream)
+    _check(L.dvdq_rms_norm_quant(*args, float(eps), _DTYPES[x.dtype], _ptr(codes), *_rows_of(codes, "codes")[1:], _ptr(x_scale),
+                                 _ptr(code_rowsum), _stream(stream)), "dvdq_rms_norm_quant")
+    return (codes, x_scale) + (() if code_rowsum is None else (code_rowsum,)) + (() if residual is None else (h,))
+
+
+def quant8(x, up=None, act: int = ACT_NONE, codes=None, x_scale=None, want_rowsum: bool = False, code_rowsum=None, stream=None):
+    """Rows of act(x) * up to 8 bits, for linear8: x [M, C] (activations, or weights with a row per channel), bf16, fp16 or fp32, rows of any
+    pitch; up like x or None.  Returns (codes int8 [M, C], x_scale fp32 [M][, code_rowsum int32 [M]]).  See dvdq_quant8."""
+    L = lib()
+    r = _marshal.quant8(x, up, act, codes, x_scale, want_rowsum, code_rowsum, stream)
+    if r is not None:
+        return _native(r, "dvdq_quant8")
+    _need_view(x, None, None, "x")
+    if x.dtype not in _DTYPES:
+        raise TypeError(f"x: expected bfloat16, float16 or float32, got {x.dtype}")
+    if x.dim() != 2:
+        raise ValueError("x: expected shape [M, C]")
+    _on_current_device(x, "x")
+    if up is not None:
+        _need_view(up, x.dtype, x.shape, "up", x.device)
+    codes, x_scale, code_rowsum = _row_codes(x, codes, x_scale, want_rowsum, code_rowsum, stream)
+    _check(L.dvdq_quant8(_ptr(x), x.stride(0), _ptr(up), 0 if up is None else up.stride(0), int(act), x.size(0), x.size(1), _DTYPES[x.dtype],
+                         _ptr(codes), codes.stride(0), _ptr(x_scale), _ptr(code_rowsum), _stream(stream)), "dvdq_quant8")
+    return (codes, x_scale) if code_rowsum is None else (codes, x_scale, code_rowsum)
+
+
+def linear8_workspace_bytes(M: int, N: int, K: int) -> int:
+    return lib().dvdq_linear8_workspace_bytes(M, N, K)
+
+
+def linear8(codes, x_scale, w, w_scale, bias=None, act: int = ACT_NONE, gate=None, residual=None, y=None, dtype=torch.bfloat16, workspace=None,
+            stream=None):
+    """y = residual + gate * act(x_scale w_scale (codes w^T) + bias), sums exact, finished in fp32, rounded once to `dtype` (bf16, fp16 or
+    fp32; y's where y is given), which is that of bias, gate and residual too.  codes: int8 [M, K] with x_scale fp32 [M] (rms_norm_quant, quant8,
+    rotate_quant with 8 bits); w: int8 [N, K] with w_scale fp32 [N] (quant8 of the weights); both with rows of any pitch; the others as for
+    linear.  Returns y [M, N].  See dvdq_linear8."""
+    L = lib()
+    r = _marshal.linear8(codes, x_scale, w, w_scale, bias, act, gate, residual, y, dtype, workspace, stream)
+    if r is not None:
+        return _native(r, "dvdq_linear8")
+    _need_view(codes, torch.int8, None, "codes")
+    if codes.dim() != 2:
+        raise ValueError("codes: expected shape [M, K]")
+    _on_current_device(codes, "codes")
+    M, K = codes.shape
+    on = codes.device
+    _need_view(w, torch.int8, None, "w", on)
+    if w.dim() != 2 or w.size(1) != K:
+        raise ValueError(f"w: expected shape [N, {K}], got {tuple(w.shape)}")
+    N = w.size(0)
+    _dense(x_scale, torch.float32, (M,), "x_scale", on)
+    _dense(w_scale, torch.float32, (N,), "w_scale", on)
+    if y is not None:
+        dtype = y.dtype if isinstance(y, torch.Tensor) else dtype
+        _need_view(y, dtype, (M, N), "y", on)
+    if dtype not in _DTYPES:
+        raise TypeError(f"dtype: expected bfloat16, float16 or float32, got {dtype}")
+    if bias is not None:
+        _need_view(bias, dtype, (N,), "bias", on)
+    gate_rows = 0
+    if gate is not None:
+        _need_view(gate, dtype, None, "gate", on)
+        gate_rows = 1 if gate.dim() == 1 else gate.size(0)
+        if gate.dim() not in (1, 2) or gate.size(-1) != N:
+            raise ValueError(f"gate: expected shape [{N}] or [G, {N}], got {tuple(gate.shape)}")
+    if residual is not None:
+        _need_view(residual, dtype, (M, N), "residual", on)
+    if y is None:
+        y = _new(lambda: torch.empty((M, N), dtype=dtype, device=on), stream)
+    workspace, n_ws = _workspace(workspace, L.dvdq_linear8_workspace_bytes(M, N, K), on, stream)
+    _check(L.dvdq_linear8(_ptr(codes), codes.stride(0), _ptr(x_scale), _ptr(w), w.stride(0), _ptr(w_scale), _ptr(bias), int(act), _ptr(gate), gate_rows,
+                          gate.stride(0) if gate_rows > 1 else N, _ptr(residual), 0 if residual is None else residual.stride(0), M, N, K,
+                          _DTYPES[dtype], _ptr(y), y.stride(0), _ptr(workspace), n_ws, _stream(stream)), "dvdq_linear8")
     return y
 
 

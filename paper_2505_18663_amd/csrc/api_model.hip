@@ -5,6 +5,7 @@
 namespace {
 
 constexpr int64_t kMaxInt = 0x7FFFFFFF;
+constexpr int64_t kMaxCodeK = 131071;   // products of any two codes then add up to less than 2^31
 constexpr int64_t kMaxTokens = (int64_t)1 << 23, kMaxChannels = (int64_t)1 << 22, kMaxPitch = (int64_t)1 << 26;   // what a launch's grid and 32-bit indices hold
 
 inline bool aligned_to(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
@@ -20,6 +21,41 @@ int check_heads(const dvdq_rope_heads *h, int64_t B, int64_t T, int dtype) {
         if (size[i] > 1 && h->in == h->out && h->in_stride[i] != h->out_stride[i]) return DVDQ_ERR_UNSUPPORTED;
     }
     if (!aligned_to(h->in, element_bytes(dtype)) || !aligned_to(h->out, element_bytes(dtype))) return DVDQ_ERR_ALIGN;
+    return DVDQ_OK;
+}
+
+// [B, S, C] rows of an output: no two at one place, and where it is `input` (NULL: none), with that one's strides
+struct Rows {
+    const void *p;
+    int64_t batch, row;
+};
+int check_out(const Rows &out, const Rows &in, int64_t B, int64_t S) {
+    if ((B > 1 && out.batch == 0) || (S > 1 && out.row == 0)) return DVDQ_ERR_UNSUPPORTED;
+    if (out.p == in.p && ((B > 1 && out.batch != in.batch) || (S > 1 && out.row != in.row))) return DVDQ_ERR_UNSUPPORTED;
+    return DVDQ_OK;
+}
+
+// What the two forms of the norm share.  y: the 16- or 32-bit output, or the codes
+int check_rms_norm(const Rows &x, const Rows &residual, const Rows &h, const void *weight, const Rows &y, bool codes, int64_t B, int64_t S, int64_t C,
+                   float eps, int dtype) {
+    if (B < 0 || S < 0 || C < 1 || !(eps >= 0.0f)) return DVDQ_ERR_SHAPE;
+    if (C > kMaxChannels || dtype < DVDQ_BF16 || dtype > DVDQ_FP32) return DVDQ_ERR_UNSUPPORTED;
+    if (B == 0 || S == 0) return DVDQ_OK;
+    if (B > kMaxInt || S > kMaxInt / B) return DVDQ_ERR_UNSUPPORTED;
+    if (!x.p || !y.p || (residual.p && !h.p)) return DVDQ_ERR_NULL;
+    if (!residual.p && h.p) return DVDQ_ERR_SHAPE;
+    const Rows none = {nullptr, 0, 0};
+    for (const Rows &in : {x, residual}) {
+        const int rc = codes ? (in.p == y.p ? (int)DVDQ_ERR_UNSUPPORTED : check_out(y, none, B, S)) : check_out(y, in, B, S);
+        if (rc != DVDQ_OK) return rc;
+        if (h.p) {
+            const int rc_h = check_out(h, in, B, S);
+            if (rc_h != DVDQ_OK) return rc_h;
+        }
+    }
+    if (h.p == y.p || (weight && (weight == y.p || weight == h.p))) return DVDQ_ERR_UNSUPPORTED;
+    for (const void *p : {x.p, residual.p, h.p, weight, codes ? nullptr : y.p})
+        if (!aligned_to(p, element_bytes(dtype))) return DVDQ_ERR_ALIGN;
     return DVDQ_OK;
 }
 
@@ -123,6 +159,69 @@ int dvdq_group_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_ba
     if (workspace_bytes < dvdq::group_norm_workspace_bytes(B, S, C, groups)) return DVDQ_ERR_WORKSPACE;
     return dvdq::launch_group_norm(x, B, S, C, x_batch, x_row, groups, weight, bias, eps, act, dtype, y, y_batch, y_row, workspace,
                                    static_cast<hipStream_t>(hip_stream));
+}
+
+int dvdq_rms_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_batch, int64_t x_row, const void *residual, int64_t r_batch,
+                  int64_t r_row, void *h, int64_t h_batch, int64_t h_row, const void *weight, float eps, int dtype, void *y, int64_t y_batch,
+                  int64_t y_row, void *hip_stream) {
+    const int rc = check_rms_norm({x, x_batch, x_row}, {residual, r_batch, r_row}, {h, h_batch, h_row}, weight, {y, y_batch, y_row}, false, B, S, C, eps, dtype);
+    if (rc != DVDQ_OK || B == 0 || S == 0) return rc;
+    return dvdq::launch_rms_norm(x, B, S, C, x_batch, x_row, residual, r_batch, r_row, h, h_batch, h_row, weight, eps, dtype, y, y_batch, y_row, nullptr,
+                                 0, 0, nullptr, nullptr, static_cast<hipStream_t>(hip_stream));
+}
+
+int dvdq_rms_norm_quant(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_batch, int64_t x_row, const void *residual, int64_t r_batch,
+                        int64_t r_row, void *h, int64_t h_batch, int64_t h_row, const void *weight, float eps, int dtype, int8_t *codes,
+                        int64_t c_batch, int64_t c_row, float *x_scale, int32_t *code_rowsum, void *hip_stream) {
+    const int rc = check_rms_norm({x, x_batch, x_row}, {residual, r_batch, r_row}, {h, h_batch, h_row}, weight, {codes, c_batch, c_row}, true, B, S, C, eps, dtype);
+    if (rc != DVDQ_OK || B == 0 || S == 0) return rc;
+    if (!x_scale) return DVDQ_ERR_NULL;
+    if (!aligned_to(x_scale, 4) || !aligned_to(code_rowsum, 4)) return DVDQ_ERR_ALIGN;
+    return dvdq::launch_rms_norm(x, B, S, C, x_batch, x_row, residual, r_batch, r_row, h, h_batch, h_row, weight, eps, dtype, nullptr, 0, 0, codes, c_batch,
+                                 c_row, x_scale, code_rowsum, static_cast<hipStream_t>(hip_stream));
+}
+
+int dvdq_quant8(const void *x, int64_t ldx, const void *up, int64_t ldu, int act, int64_t M, int64_t C, int dtype, int8_t *codes, int64_t ldc,
+                float *x_scale, int32_t *code_rowsum, void *hip_stream) {
+    if (M < 0 || C < 1) return DVDQ_ERR_SHAPE;
+    if (C > kMaxChannels || M > kMaxInt || act < DVDQ_ACT_NONE || act > DVDQ_ACT_GELU || dtype < DVDQ_BF16 || dtype > DVDQ_FP32) return DVDQ_ERR_UNSUPPORTED;
+    if (M == 0) return DVDQ_OK;
+    if (!x || !codes || !x_scale) return DVDQ_ERR_NULL;
+    if (M > 1 && ldc < C) return DVDQ_ERR_SHAPE;
+    if (codes == x || codes == up) return DVDQ_ERR_UNSUPPORTED;
+    if (!aligned_to(x, element_bytes(dtype)) || !aligned_to(up, element_bytes(dtype)) || !aligned_to(x_scale, 4) || !aligned_to(code_rowsum, 4)) return DVDQ_ERR_ALIGN;
+    return dvdq::launch_quant8(x, ldx, up, ldu, act, M, C, dtype, codes, ldc, x_scale, code_rowsum, static_cast<hipStream_t>(hip_stream));
+}
+
+size_t dvdq_linear8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    if (M < 1 || N < 1 || K < 1 || M > kMaxTokens || N > kMaxChannels || K > kMaxCodeK) return 0;
+    return dvdq::linear8_workspace_bytes(M, N, K);
+}
+
+int dvdq_linear8(const int8_t *codes, int64_t ldc, const float *x_scale, const int8_t *w, int64_t ldw, const float *w_scale, const void *bias, int act,
+                 const void *gate, int64_t gate_rows, int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype,
+                 void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (M < 0 || N < 1 || K < 1) return DVDQ_ERR_SHAPE;
+    if (M == 0) return DVDQ_OK;
+    if (!codes || !x_scale || !w || !w_scale || !y) return DVDQ_ERR_NULL;
+    if (gate && (gate_rows < 1 || M % gate_rows)) return DVDQ_ERR_SHAPE;
+    if ((M > 1 && (ldc < K || ldy < N || (residual && ldr < N))) || (N > 1 && ldw < K) || (gate && gate_rows > 1 && ldg < N)) return DVDQ_ERR_SHAPE;
+    if (M > kMaxTokens || N > kMaxChannels || K > kMaxCodeK || act < DVDQ_ACT_NONE || act > DVDQ_ACT_GELU || dtype < DVDQ_BF16 || dtype > DVDQ_FP32 ||
+        (residual == y && M > 1 && ldr != ldy) || (M > 1 && (ldy > kMaxPitch || (residual && ldr > kMaxPitch))))
+        return DVDQ_ERR_UNSUPPORTED;
+    // operands of which other outputs still need what an output would overwrite
+    if (y == codes || y == w || y == x_scale || y == w_scale || (y == bias && M > 1) || (y == gate && (gate_rows != M || (M > 1 && ldg != ldy)))) return DVDQ_ERR_UNSUPPORTED;
+    for (const void *p : {bias, gate, residual, static_cast<const void *>(y)})
+        if (!aligned_to(p, element_bytes(dtype))) return DVDQ_ERR_ALIGN;
+    if (!aligned_to(x_scale, 4) || !aligned_to(w_scale, 4)) return DVDQ_ERR_ALIGN;
+    const size_t need = dvdq::linear8_workspace_bytes(M, N, K);
+    if (need) {
+        if (!workspace) return DVDQ_ERR_NULL;
+        if (!aligned_to(workspace, 16)) return DVDQ_ERR_ALIGN;
+        if (workspace_bytes < need) return DVDQ_ERR_WORKSPACE;
+    }
+    return dvdq::launch_linear8(codes, ldc, x_scale, w, ldw, w_scale, bias, act, gate, gate_rows, ldg, residual, ldr, M, N, K, dtype, y, ldy, workspace,
+                                static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

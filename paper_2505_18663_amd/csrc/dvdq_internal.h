@@ -175,6 +175,17 @@ int launch_group_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_
                       const void *bias, float eps, int act, int dtype, void *y, int64_t y_batch, int64_t y_row, void *workspace,
                       hipStream_t stream);
 
+// Norms and layers in 8 bits (rows8.hip, linear8.hip); likewise
+int launch_rms_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_batch, int64_t x_row, const void *residual, int64_t r_batch,
+                    int64_t r_row, void *h, int64_t h_batch, int64_t h_row, const void *weight, float eps, int dtype, void *y, int64_t y_batch,
+                    int64_t y_row, int8_t *codes, int64_t c_batch, int64_t c_row, float *x_scale, int32_t *code_rowsum, hipStream_t stream);
+int launch_quant8(const void *x, int64_t ldx, const void *up, int64_t ldu, int act, int64_t M, int64_t C, int dtype, int8_t *codes, int64_t ldc,
+                  float *x_scale, int32_t *code_rowsum, hipStream_t stream);
+size_t linear8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int launch_linear8(const int8_t *codes, int64_t ldc, const float *x_scale, const int8_t *w, int64_t ldw, const float *w_scale, const void *bias, int act,
+                   const void *gate, int64_t gate_rows, int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype,
+                   void *y, int64_t ldy, void *workspace, hipStream_t stream);
+
 // Raise a kernel's dynamic-LDS limit to `bytes` once per kernel and device (`done` is the call
 // site's own bit mask of devices already configured).  Not a stream operation: after the first
 // launch on a device nothing but the launch itself is issued, also under stream capture.

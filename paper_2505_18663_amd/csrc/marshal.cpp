@@ -15,6 +15,8 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/StreamGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
+#include <torch/csrc/Dtype.h>
 
 #include <optional>
 
@@ -37,6 +39,11 @@ decltype(&dvdq_linear) p_linear;
 decltype(&dvdq_linear_workspace_bytes) p_linear_workspace_bytes;
 decltype(&dvdq_group_norm) p_group_norm;
 decltype(&dvdq_group_norm_workspace_bytes) p_group_norm_workspace_bytes;
+decltype(&dvdq_rms_norm) p_rms_norm;
+decltype(&dvdq_rms_norm_quant) p_rms_norm_quant;
+decltype(&dvdq_quant8) p_quant8;
+decltype(&dvdq_linear8) p_linear8;
+decltype(&dvdq_linear8_workspace_bytes) p_linear8_workspace_bytes;
 
 PyObject *get_device, *get_raw_stream;   // torch._C's: number of the current device; its current stream's handle
 
@@ -480,16 +487,217 @@ PyObject *group_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// ---- layers in 8 bits.  Launches go to the current device: tensors of another one are handed back, to be refused.
+bool on_current_device(const at::Tensor &t) { return c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice() == t.device(); }
+
+// rows of a tensor [M, C] (M batches of one row) or [B, S, C]
+struct RowsOf {
+    int64_t batch, row;
+    explicit RowsOf(const at::Tensor *t) : batch(t ? t->stride(0) : 0), row(!t ? 0 : t->dim() == 3 ? t->stride(1) : t->size(1)) {}
+};
+
+// x, weight, residual of the norm and where their sum goes; new tensors are the guard's stream's
+struct NormRows {
+    const at::Tensor *x, *weight, *residual;
+    at::Tensor h;
+    int type = -1;
+    int64_t B = 0, S = 0, C = 0;
+
+    NormRows(Args &a, int dim) {
+        x = a.view(0, dim, nullptr), weight = a.view(1, 1, x, true), residual = a.view(2, dim, x, true);
+        type = a.ok ? Args::type_of(*x) : -1;
+        a.require(type >= 0);
+        if (!a.ok) return;
+        B = x->size(0), S = dim == 3 ? x->size(1) : 1, C = x->size(dim - 1);
+        a.require((!weight || weight->size(0) == C) && (!residual || residual->sizes() == x->sizes()) && (residual || a.none(4)) && on_current_device(*x));
+    }
+    void sum(Args &a, const std::optional<c10::StreamGuard> &guard) {
+        if (residual && a.ok) h = a.output_like(4, x->sizes(), *x, guard);
+    }
+};
+
+// a given dense tensor of that shape, or a new one; likewise
+at::Tensor dense(Args &a, int i, at::ScalarType type, at::IntArrayRef shape, const at::Tensor &like, const std::optional<c10::StreamGuard> &guard) {
+    if (a.none(i)) {
+        at::Tensor t = at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
+        if (guard) t.record_stream(guard->original_stream());
+        return t;
+    }
+    const at::Tensor *t = a.tensor(i, type);
+    a.require(t && t->sizes() == shape && t->device() == like.device());
+    return a.ok ? *t : at::Tensor();
+}
+
+// codes (a view), x_scale, code_rowsum at arguments i, i + 1, i + 3; whether sums are wanted at i + 2
+struct RowCodes {
+    at::Tensor codes, scale, sums;
+    int at;
+
+    RowCodes(Args &a, int i, const at::Tensor &x, const std::optional<c10::StreamGuard> &guard) : at(i) {
+        a.require(a.a[i + 2] == Py_True || a.a[i + 2] == Py_False);
+        if (a.ok && !a.none(i)) {
+            const at::Tensor *t = a.view(i, x.dim(), nullptr);
+            a.require(t && t->scalar_type() == at::kChar && t->sizes() == x.sizes() && t->device() == x.device());
+            if (a.ok) codes = *t;
+        } else if (a.ok) {
+            codes = dense(a, i, at::kChar, x.sizes(), x, guard);
+        }
+        const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
+        if (a.ok) scale = dense(a, i + 1, at::kFloat, lead, x, guard);
+        if (a.ok && (a.a[i + 2] == Py_True || !a.none(i + 3))) sums = dense(a, i + 3, at::kInt, lead, x, guard);
+    }
+    // (codes, x_scale[, code_rowsum][, h])
+    PyObject *result(PyObject *const *args, PyObject *h) const {
+        PyObject *c = object(args[at], codes), *s = object(args[at + 1], scale);
+        if (sums.defined()) {
+            PyObject *r = object(args[at + 3], sums);
+            return h ? Py_BuildValue("(NNNN)", c, s, r, h) : Py_BuildValue("(NNN)", c, s, r);
+        }
+        return h ? Py_BuildValue("(NNN)", c, s, h) : Py_BuildValue("(NN)", c, s);
+    }
+};
+
+// [M, C] or [B, S, C]; tensors of more dimensions are handed back
+int rows_dim(PyObject *x) {
+    const int64_t dim = THPVariable_CheckExact(x) ? THPVariable_Unpack(x).dim() : 0;
+    return dim == 2 || dim == 3 ? (int)dim : 0;
+}
+
+// x, weight, residual, eps, h, y, stream -> y or (y, h)
+PyObject *rms_norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 7);
+    const int dim = a.ok ? rows_dim(args[0]) : 0;
+    if (!dim || !PyFloat_CheckExact(args[3])) Py_RETURN_NONE;
+    NormRows r(a, dim);
+    std::optional<c10::StreamGuard> guard;
+    void *stream = a.stream(6, guard);
+    r.sum(a, guard);
+    if (!a.ok) Py_RETURN_NONE;
+    const at::Tensor y = a.output_like(5, r.x->sizes(), *r.x, guard);
+    if (!a.ok) Py_RETURN_NONE;
+    const at::Tensor *h = r.residual ? &r.h : nullptr;
+    const RowsOf x(r.x), res(r.residual), hr(h), yr(&y);
+    const float eps = (float)PyFloat_AS_DOUBLE(args[3]);
+    const int rc = unlocked([&] {
+        return p_rms_norm(r.x->data_ptr(), r.B, r.S, r.C, x.batch, x.row, ptr(r.residual), res.batch, res.row, ptr(h), hr.batch, hr.row, ptr(r.weight), eps,
+                          r.type, y.data_ptr(), yr.batch, yr.row, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    if (h) return Py_BuildValue("(NN)", object(args[5], y), object(args[4], *h));
+    return object(args[5], y);
+    END_HANDLE_TH_ERRORS
+}
+
+// x, weight, residual, eps, h, codes, x_scale, want_rowsum, code_rowsum, stream -> (codes, x_scale[, code_rowsum][, h])
+PyObject *rms_norm_quant(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 10);
+    const int dim = a.ok ? rows_dim(args[0]) : 0;
+    if (!dim || !PyFloat_CheckExact(args[3])) Py_RETURN_NONE;
+    NormRows r(a, dim);
+    std::optional<c10::StreamGuard> guard;
+    void *stream = a.stream(9, guard);
+    r.sum(a, guard);
+    if (!a.ok) Py_RETURN_NONE;
+    const RowCodes o(a, 5, *r.x, guard);
+    if (!a.ok) Py_RETURN_NONE;
+    const at::Tensor *h = r.residual ? &r.h : nullptr;
+    const RowsOf x(r.x), res(r.residual), hr(h), c(&o.codes);
+    const float eps = (float)PyFloat_AS_DOUBLE(args[3]);
+    const int rc = unlocked([&] {
+        return p_rms_norm_quant(r.x->data_ptr(), r.B, r.S, r.C, x.batch, x.row, ptr(r.residual), res.batch, res.row, ptr(h), hr.batch, hr.row, ptr(r.weight),
+                                eps, r.type, (int8_t *)o.codes.data_ptr(), c.batch, c.row, (float *)o.scale.data_ptr(),
+                                o.sums.defined() ? (int32_t *)o.sums.data_ptr() : nullptr, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return o.result(args, h ? object(args[4], *h) : nullptr);
+    END_HANDLE_TH_ERRORS
+}
+
+// x, up, act, codes, x_scale, want_rowsum, code_rowsum, stream -> (codes, x_scale[, code_rowsum])
+PyObject *quant8(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 8);
+    const at::Tensor *x = a.view(0, 2, nullptr), *up = a.view(1, 2, x, true);
+    const int act = a.small(2), type = a.ok ? Args::type_of(*x) : -1;
+    if (!a.ok || type < 0 || (up && up->sizes() != x->sizes()) || !on_current_device(*x)) Py_RETURN_NONE;
+    std::optional<c10::StreamGuard> guard;
+    void *stream = a.stream(7, guard);
+    if (!a.ok) Py_RETURN_NONE;
+    const RowCodes o(a, 3, *x, guard);
+    if (!a.ok) Py_RETURN_NONE;
+    const int rc = unlocked([&] {
+        return p_quant8(x->data_ptr(), x->stride(0), ptr(up), up ? up->stride(0) : 0, act, x->size(0), x->size(1), type, (int8_t *)o.codes.data_ptr(),
+                        o.codes.stride(0), (float *)o.scale.data_ptr(), o.sums.defined() ? (int32_t *)o.sums.data_ptr() : nullptr, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return o.result(args, nullptr);
+    END_HANDLE_TH_ERRORS
+}
+
+// codes, x_scale, w, w_scale, bias, act, gate, residual, y, dtype, workspace, stream -> y
+PyObject *linear8(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Args a(args, n, 12);
+    const at::Tensor *x = a.view(0, 2, nullptr), *w = a.view(2, 2, x), *x_scale = a.tensor(1, at::kFloat), *w_scale = a.tensor(3, at::kFloat);
+    const int act = a.small(5);
+    if (!a.ok || x->scalar_type() != at::kChar || !on_current_device(*x) || x_scale->device() != x->device() || w_scale->device() != x->device())
+        Py_RETURN_NONE;
+    const int64_t M = x->size(0), K = x->size(1), N = w->size(0);
+    if (w->size(1) != K || !vector_of(x_scale, M) || !vector_of(w_scale, N)) Py_RETURN_NONE;
+    // the type of the output, and of what goes into the epilogue
+    at::ScalarType type;
+    if (!a.none(8)) {
+        if (!THPVariable_CheckExact(args[8])) Py_RETURN_NONE;
+        type = THPVariable_Unpack(args[8]).scalar_type();
+    } else {
+        if (!THPDtype_Check(args[9])) Py_RETURN_NONE;
+        type = reinterpret_cast<THPDtype *>(args[9])->scalar_type;
+    }
+    const int code = type == at::kBFloat16 ? DVDQ_BF16 : type == at::kHalf ? DVDQ_FP16 : type == at::kFloat ? DVDQ_FP32 : -1;
+    const auto of_type = [&](const at::Tensor *t) { return !t || (t->scalar_type() == type && t->device() == x->device()); };
+    const at::Tensor *bias = a.view(4, 1, nullptr, true), *res = a.view(7, 2, nullptr, true), *gate = nullptr;
+    if (a.ok && !a.none(6)) gate = a.view(6, THPVariable_CheckExact(args[6]) && THPVariable_Unpack(args[6]).dim() == 1 ? 1 : 2, nullptr);
+    if (!a.ok || code < 0 || !of_type(bias) || !of_type(gate) || !of_type(res) || (bias && bias->size(0) != N) || (gate && gate->size(gate->dim() - 1) != N) ||
+        (res && (res->size(0) != M || res->size(1) != N)))
+        Py_RETURN_NONE;
+    std::optional<c10::StreamGuard> guard;
+    void *stream = a.stream(11, guard);
+    if (!a.ok) Py_RETURN_NONE;
+    at::Tensor y;
+    if (a.none(8)) {
+        y = dense(a, 8, type, {M, N}, *x, guard);
+    } else {
+        const at::Tensor *t = a.view(8, 2, nullptr);
+        if (!t || !of_type(t) || t->size(0) != M || t->size(1) != N) Py_RETURN_NONE;
+        y = *t;
+    }
+    const at::Tensor ws = a.scratch(10, a.none(10) ? p_linear8_workspace_bytes(M, N, K) : 0, *x);
+    if (!a.ok) Py_RETURN_NONE;
+    const int64_t gate_rows = gate ? (gate->dim() == 1 ? 1 : gate->size(0)) : 0;
+    const int rc = unlocked([&] {
+        return p_linear8((const int8_t *)x->data_ptr(), x->stride(0), (const float *)x_scale->data_ptr(), (const int8_t *)w->data_ptr(), w->stride(0),
+                         (const float *)w_scale->data_ptr(), ptr(bias), act, ptr(gate), gate_rows, gate_rows > 1 ? gate->stride(0) : N, ptr(res),
+                         res ? res->stride(0) : 0, M, N, K, code, y.data_ptr(), y.stride(0), ws.defined() ? ws.data_ptr() : nullptr,
+                         ws.defined() ? (size_t)ws.numel() : 0, stream);
+    });
+    if (rc != 0) return PyLong_FromLong(rc);
+    return object(args[8], y);
+    END_HANDLE_TH_ERRORS
+}
+
 // torch._C._cuda_getDevice and _cuda_getCurrentRawStream, then the addresses of the C functions in the library that the binding has
 // loaded, in this order.
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
     void **const to[] = {(void **)&p_rotate_quant, (void **)&p_rotate_quant_blockwise, (void **)&p_w4ax_gemm, (void **)&p_qlinear,
                          (void **)&p_gbs_reset, (void **)&p_gbs_step, (void **)&p_codes_bytes, (void **)&p_qlinear_workspace_bytes,
                          (void **)&p_w4_native_bytes, (void **)&p_w4_native_fp6_bytes, (void **)&p_rope, (void **)&p_linear,
-                         (void **)&p_linear_workspace_bytes, (void **)&p_group_norm, (void **)&p_group_norm_workspace_bytes};
+                         (void **)&p_linear_workspace_bytes, (void **)&p_group_norm, (void **)&p_group_norm_workspace_bytes,
+                         (void **)&p_rms_norm, (void **)&p_rms_norm_quant, (void **)&p_quant8, (void **)&p_linear8, (void **)&p_linear8_workspace_bytes};
     constexpr Py_ssize_t kFunctions = sizeof(to) / sizeof(to[0]);
     if (n != 2 + kFunctions) {
-        PyErr_SetString(PyExc_TypeError, "bind: two callables and fifteen addresses");
+        PyErr_SetString(PyExc_TypeError, "bind: two callables and twenty addresses");
         return nullptr;
     }
     Py_INCREF(args[0]);
@@ -506,7 +714,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
 #define DVDQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DVDQ_METHOD(bind), DVDQ_METHOD(qlinear), DVDQ_METHOD(rotate_quant), DVDQ_METHOD(rotate_quant_blockwise),
                          DVDQ_METHOD(w4ax_gemm), DVDQ_METHOD(gbs_reset), DVDQ_METHOD(gbs_step), DVDQ_METHOD(rope), DVDQ_METHOD(linear),
-                         DVDQ_METHOD(group_norm), {nullptr, nullptr, 0, nullptr}};
+                         DVDQ_METHOD(group_norm), DVDQ_METHOD(rms_norm), DVDQ_METHOD(rms_norm_quant), DVDQ_METHOD(quant8), DVDQ_METHOD(linear8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
