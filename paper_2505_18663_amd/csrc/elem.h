@@ -46,7 +46,14 @@ static __device__ __forceinline__ Piece<E, V> load_piece(const typename E::Raw *
 template <typename E, int V = E::kVec, bool STREAM = false>
 static __device__ __forceinline__ void store_piece(typename E::Raw *p, const Piece<E, V> &v, int n) {
     if (n >= V) {
-        if constexpr (STREAM && sizeof(v) == 16) {
+        if constexpr (STREAM && sizeof(v) == 32) {   // (fp32: two pieces)
+            typedef uint32_t Quad __attribute__((ext_vector_type(4)));
+            typedef Quad Anywhere __attribute__((aligned(4)));
+            struct Two { Quad q[2]; };
+            const Two t = __builtin_bit_cast(Two, v);
+            __builtin_nontemporal_store(t.q[0], reinterpret_cast<Anywhere *>(p));
+            __builtin_nontemporal_store(t.q[1], reinterpret_cast<Anywhere *>(p) + 1);
+        } else if constexpr (STREAM && sizeof(v) == 16) {
             typedef uint32_t Quad __attribute__((ext_vector_type(4)));
             typedef Quad Anywhere __attribute__((aligned(2)));
             __builtin_nontemporal_store(__builtin_bit_cast(Quad, v), reinterpret_cast<Anywhere *>(p));
