@@ -8,6 +8,8 @@
 //
 // Codes are those of the real numbers: values next to the border between two codes are worked out again in 64 bits (a product of two
 // 24-bit numbers is exact there), so codes depend neither on the launch nor on how well fp32 activations are computed.
+#include <algorithm>
+
 #include "elem.h"
 #include "wave_reduce.h"
 
@@ -23,12 +25,17 @@ struct RowArgs {
     int32_t *rowsum;
     int64_t x_batch, x_row, s_batch, s_row, h_batch, h_row, y_batch, y_row, c_batch, c_row;
     int64_t rows;
-    uint32_t S;                                      // rows of a batch
+    uint32_t S, S_mul, S_shift;                      // rows of a batch; row / S = row * S_mul >> 32 + S_shift for rows below 2^31 (S > 1)
     int C, act;
     float eps;
 };
 
-enum { kNorm = 0, kNormCodes = 1, kQuant = 2 };
+struct Code {
+    using Raw = int8_t;
+};
+
+enum { kNorm = 0, kNormCodes = 1, kQuant = 2, kQuantAct = 3 };   // (kQuantAct: with an activation)
+constexpr bool is_norm(int mode) { return mode <= kNormCodes; }
 
 static __device__ __forceinline__ float act32(float z, int act) {
     switch (act) {
@@ -39,7 +46,7 @@ static __device__ __forceinline__ float act32(float z, int act) {
     }
 }
 
-static __device__ __noinline__ double act64(double z, int act) {
+static __device__ __forceinline__ double act64(double z, int act) {
     switch (act) {
         case DVDQ_ACT_SILU: return z / (1.0 + exp(-z));
         case DVDQ_ACT_GELU_TANH: return z / (1.0 + exp(-1.5957691216057308 * (z + 0.044715 * z * z * z)));
@@ -48,108 +55,316 @@ static __device__ __noinline__ double act64(double z, int act) {
     }
 }
 
-// Reductions over a workgroup; every thread gets the result.
-template <class T, class Op>
-static __device__ __forceinline__ T all(T v, T *lds, Op op) {
+// A row's elements: h or x, and z in 32 and in 64 bits
+template <typename E, int MODE>
+struct Row {
+    using Raw = typename E::Raw;
+    static constexpr bool kWide = sizeof(Raw) == 4;
+    const Raw *x, *second, *weight;
+    Raw *h, *y;
+    int8_t *codes;
+    int act;
+    bool exact;                                      // fp32 holds z as it is: a product of two 16-bit values, or no product
+
+    __device__ __forceinline__ Row(const RowArgs &a, uint32_t row) {
+        const int64_t b = a.S == 1 ? row : __umulhi(row, a.S_mul) >> a.S_shift, s = row - (uint32_t)b * a.S;
+        x = static_cast<const Raw *>(a.x) + b * a.x_batch + s * a.x_row;
+        second = a.second ? static_cast<const Raw *>(a.second) + b * a.s_batch + s * a.s_row : nullptr;
+        weight = static_cast<const Raw *>(a.weight);
+        h = a.h ? static_cast<Raw *>(a.h) + b * a.h_batch + s * a.h_row : nullptr;
+        y = static_cast<Raw *>(a.y) + b * a.y_batch + s * a.y_row;
+        codes = a.codes + b * a.c_batch + s * a.c_row;
+        act = a.act;
+        exact = MODE == kQuantAct ? false : !kWide || !(is_norm(MODE) ? weight : second);
+    }
+    // the value that z is made of, from memory; summed: h is there already
+    __device__ __forceinline__ float value(int c, bool summed) const {
+        if (is_norm(MODE) && second) return E::to_f32(summed ? h[c] : E::from_f32(E::to_f32(x[c]) + E::to_f32(second[c])));
+        return E::to_f32(x[c]);
+    }
+    __device__ __forceinline__ float z32(int c, float v) const {
+        if (MODE == kQuantAct) v = act32(v, act);
+        if (!is_norm(MODE)) return second ? v * E::to_f32(second[c]) : v;
+        return weight ? v * E::to_f32(weight[c]) : v;
+    }
+    __device__ __forceinline__ double z64(int c, float v) const {
+        if (!is_norm(MODE)) return (MODE == kQuantAct ? act64(v, act) : (double)v) * (second ? (double)E::to_f32(second[c]) : 1.0);
+        return weight ? (double)v * E::to_f32(weight[c]) : (double)v;
+    }
+    // How far fp32 may have 127 z / max|z| = t off.  The quotient 127 / max|z| is off by 2^-24, products by 2^-24, activations by 2^-20 of themselves
+    // and by up to 2^-15 where they fall like an exponential (see activate); v: the activation's argument.
+    __device__ __forceinline__ float margin(float t, float v) const {
+        if (MODE != kQuantAct) return exact ? 0x1p-16f : 0x1p-15f;
+        return 0x1p-15f + fabsf(t) * (v < -2.0f ? 0x1p-15f : 0x1p-18f);
+    }
+};
+constexpr float kTiny = 0x1p-60f;                    // below, products in fp32 may have lost digits
+constexpr float kNearTop = 1.0f - 0x1p-13f;          // what may turn out to be the largest, as a share of the largest in fp32
+
+// Reductions over the T threads of a row (8 to 1024); every thread gets the result.  Beyond a wave through LDS, whose two halves take turns (`turn`).
+template <int T, class V, class Op>
+static __device__ __forceinline__ V over_row(V v, Op op, uint64_t *lds, int &turn) {
+    v = op(v, dpp<DPP_XOR1>(v));
+    v = op(v, dpp<DPP_XOR2>(v));
+    v = op(v, dpp<DPP_HALF_MIRROR>(v));
+    if constexpr (T >= 16) v = op(v, dpp<DPP_MIRROR>(v));
+    if constexpr (T >= 32) v = swap_rows<false>(v, op);
+    if constexpr (T >= 64) v = swap_rows<true>(v, op);
+    if constexpr (T > 64) {
+        V *slots = reinterpret_cast<V *>(lds + (turn ^= 16));
+        if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = v;
+        __syncthreads();
+        V w[T / 64];
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) v = op(v, __shfl_xor(v, m));
-    const int waves = blockDim.x >> 6;
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-    for (int i = 1; i < waves; ++i) v = op(v, lds[i]);
-    __syncthreads();
+        for (int i = 0; i < T / 64; ++i) w[i] = slots[i];
+        v = w[0];
+#pragma unroll
+        for (int i = 1; i < T / 64; ++i) v = op(v, w[i]);
+    }
     return v;
 }
+struct Add {
+    template <class V>
+    __device__ V operator()(V a, V b) const { return a + b; }
+};
+struct Larger {
+    template <class V>
+    __device__ V operator()(V a, V b) const { return a > b ? a : b; }
+};
 
-// A workgroup per row, which it reads again for each step.
-template <typename E, int MODE>
-__global__ __launch_bounds__(256) void row_any(RowArgs a) {
-    using Raw = typename E::Raw;
-    constexpr bool WIDE = sizeof(Raw) == 4;
-    __shared__ double lds[4];
-    const auto add = [](auto p, auto q) { return p + q; };
-    const auto larger = [](auto p, auto q) { return p > q ? p : q; };
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const int64_t b = (uint32_t)row / a.S, s = (uint32_t)row % a.S;
-        const Raw *x = static_cast<const Raw *>(a.x) + b * a.x_batch + s * a.x_row;
-        const Raw *second = a.second ? static_cast<const Raw *>(a.second) + b * a.s_batch + s * a.s_row : nullptr;
-        const Raw *weight = static_cast<const Raw *>(a.weight);
-        const bool plain = MODE == kQuant && a.act == DVDQ_ACT_NONE;
-        // whether fp32 holds z as it is: a product of two 16-bit values, or no product
-        const bool exact = MODE == kQuant ? plain && (!WIDE || !second) : !WIDE || !weight;
-        auto value = [&](int c) {
-            float v = E::to_f32(x[c]);
-            if (MODE != kQuant && second) v = E::to_f32(E::from_f32(v + E::to_f32(second[c])));
-            return v;
-        };
-        auto z32 = [&](int c, float v) {
-            if (MODE == kQuant) return act32(v, a.act) * (second ? E::to_f32(second[c]) : 1.0f);
-            return weight ? v * E::to_f32(weight[c]) : v;
-        };
-        auto z64 = [&](int c, float v) {
-            if (MODE == kQuant) return act64(v, a.act) * (second ? (double)E::to_f32(second[c]) : 1.0);
-            return weight ? (double)v * E::to_f32(weight[c]) : (double)v;
-        };
-        float sum = 0.0f;
+// What becomes of a row once its largest |z| is known in fp32
+struct Scale {
+    double top;      // max|z|
+    float reach;     // 127 / top
+    bool fine, tiny; // no NaN or infinity; products may have lost digits
+};
+static __device__ __forceinline__ float scale_of(const Scale &s, float factor) {
+    return !s.fine ? __builtin_nanf("") : s.top > 0.0 ? (float)(s.top / 127.0) * factor : 0.0f;
+}
+static __device__ __forceinline__ Scale scale_from(uint32_t top_bits) {
+    const float top = __builtin_bit_cast(float, top_bits);
+    return {(double)top, 0.0f, top_bits < 0x7F800000u, top < kTiny};
+}
+
+// T threads a row, which they hold: NP pieces of 16 bytes each.
+template <typename E, int MODE, int T, int NP>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
+    constexpr int V = E::kVec, R = T < 256 ? 256 / T : 1;
+    __shared__ uint64_t lds[32];
+    int turn = 0;
+    const int l = threadIdx.x % T;
+    for (int64_t row0 = (int64_t)blockIdx.x * R; row0 < a.rows; row0 += (int64_t)gridDim.x * R) {
+        const int64_t mine = row0 + threadIdx.x / T;
+        const bool there = R == 1 || mine < a.rows;
+        uint32_t row = (uint32_t)(there ? mine : a.rows - 1);
+        if (T >= 64) row = __builtin_amdgcn_readfirstlane(row);
+        const Row<E, MODE> r(a, row);
+        Piece<E> px[NP], ps[NP], pw[NP];
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int c = (l + T * i) * V, n = a.C - c;
+            px[i] = load_piece<E>(r.x + c, n);
+            if (r.second) ps[i] = load_piece<E>(r.second + c, n);
+            if (is_norm(MODE) && r.weight) pw[i] = load_piece<E>(r.weight + c, n);
+        }
+        float z[NP][V], sum = 0.0f;
         uint32_t top_bits = 0;
-        for (int c = threadIdx.x; c < a.C; c += 256) {
-            const float v = value(c);
-            if (MODE != kQuant) sum += v * v;
-            if (MODE != kNorm) top_bits = max(top_bits, __builtin_bit_cast(uint32_t, z32(c, v)) & 0x7FFFFFFFu);   // (a NaN is above infinity)
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int c = (l + T * i) * V, n = a.C - c;
+            if (!is_norm(MODE)) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) z[i][e] = MODE == kQuantAct ? act32(E::to_f32(px[i].e[e]), r.act) : E::to_f32(px[i].e[e]);
+                if (r.second)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) z[i][e] *= E::to_f32(ps[i].e[e]);
+            } else {
+                if (r.second) {
+#pragma unroll
+                    for (int e = 0; e < V; ++e) px[i].e[e] = E::from_f32(E::to_f32(px[i].e[e]) + E::to_f32(ps[i].e[e]));
+                    if (there) store_piece<E>(r.h + c, px[i], n);
+                }
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    z[i][e] = E::to_f32(px[i].e[e]);
+                    sum += z[i][e] * z[i][e];
+                }
+                if (r.weight)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) z[i][e] *= E::to_f32(pw[i].e[e]);
+            }
+            if (MODE != kNorm)
+#pragma unroll
+                for (int e = 0; e < V; ++e) top_bits = max(top_bits, __builtin_bit_cast(uint32_t, z[i][e]) & 0x7FFFFFFFu);   // (a NaN is above infinity)
         }
         float factor = 1.0f;
-        if (MODE != kQuant) factor = 1.0f / sqrtf(all(sum, reinterpret_cast<float *>(lds), add) / (float)a.C + a.eps);
-        double top = 0.0;
-        bool fine = true, tiny = false;
-        if (MODE != kNorm) {
-            top_bits = all(top_bits, reinterpret_cast<uint32_t *>(lds), larger);
-            const float top32 = __builtin_bit_cast(float, top_bits);
-            fine = top_bits < 0x7F800000u;
-            top = top32;
-            tiny = top32 < 0x1p-60f;                 // (products of small numbers: fp32 may have lost digits)
-            if (fine && (!exact || tiny)) {
-                const float near = tiny ? 0.0f : top32 * (1.0f - 0x1p-13f);
-                double t = 0.0;
-                for (int c = threadIdx.x; c < a.C; c += 256) {
-                    const float v = value(c);
-                    if (fabsf(z32(c, v)) >= near) t = larger(t, fabs(z64(c, v)));
-                }
-                top = all(t, lds, larger);
+        if (is_norm(MODE)) factor = 1.0f / sqrtf(over_row<T>(sum, Add(), lds, turn) / (float)a.C + a.eps);
+        if (MODE == kNorm) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int c = (l + T * i) * V, n = a.C - c;
+                Piece<E> o;
+#pragma unroll
+                for (int e = 0; e < V; ++e) o.e[e] = E::from_f32(z[i][e] * factor);
+                if (there) store_piece<E>(r.y + c, o, n);
             }
+            continue;
         }
-        const float reach = top > 0.0 ? (float)(127.0 / top) : 0.0f;
-        int codes = 0;
-        for (int c = threadIdx.x; c < a.C; c += 256) {
-            const float v = value(c);
-            if (MODE != kQuant && a.h) static_cast<Raw *>(a.h)[b * a.h_batch + s * a.h_row + c] = E::from_f32(v);
+        // Which of a thread's elements need a second look: bit V i + e.  That goes by the values in memory, so that there is one place for it.
+        static_assert(NP * V <= 32, "a bit each");
+        const auto place = [&](uint32_t bit) { return (l + T * (int)(bit / V)) * V + (int)(bit % V); };
+        Scale s = scale_from(over_row<T>(top_bits, Larger(), lds, turn));
+        if (!r.exact || s.tiny) {
+            double t = 0.0;
+            if (s.fine) {
+                const float near = s.tiny ? 0.0f : (float)s.top * kNearTop;
+                uint32_t which = 0;
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) which |= (fabsf(z[i][e]) >= near ? 1u : 0u) << (V * i + e);
+                for (; which; which &= which - 1) {
+                    const int c = place(__builtin_ctz(which));
+                    if (c < a.C) t = Larger()(t, fabs(r.z64(c, r.value(c, true))));
+                }
+            }
+            t = over_row<T>(t, Larger(), lds, turn);
+            if (s.fine) s.top = t;
+        }
+        s.reach = s.top > 0.0 ? (float)(127.0 / s.top) : 0.0f;
+        int total = 0;
+        uint32_t near = 0;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int c = (l + T * i) * V, n = a.C - c;
+            // t + 1.5 2^23 has the whole number next to t in its lowest bits
+            constexpr float kMagic = 12582912.0f;
+            Piece<Code, V> o;
+            int word[V / 4];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float m = fmaf(z[i][e], s.reach, kMagic), q = m - kMagic, off = fmaf(z[i][e], s.reach, -q);
+                near |= (fabsf(off) > 0.5f - r.margin(q, MODE == kQuantAct ? E::to_f32(px[i].e[e]) : 0.0f) ? 1u : 0u) << (V * i + e);
+                o.e[e] = s.fine ? (int8_t)__builtin_bit_cast(uint32_t, m) : 0;
+            }
+            if (there) store_piece<Code, V>(r.codes + c, o, n);
+            __builtin_memcpy(word, &o, V);
+#pragma unroll
+            for (int w = 0; w < V / 4; ++w) total = __builtin_amdgcn_sdot4(word[w], 0x01010101, total, false);
+        }
+        if (s.fine && s.top > 0.0)
+            for (near = s.tiny ? ~0u >> (32 - NP * V) : near; near; near &= near - 1) {
+                const int c = place(__builtin_ctz(near));
+                if (c >= a.C) break;
+                const int code = (int)rint(127.0 * r.z64(c, r.value(c, true)) / s.top);
+                if (there) {
+                    total += code - r.codes[c];
+                    r.codes[c] = (int8_t)code;
+                }
+            }
+        if (a.rowsum) {
+            total = over_row<T>(total, Add(), lds, turn);
+            if (l == 0 && there) a.rowsum[row] = total;
+        }
+        if (l == 0 && there) a.scale[row] = scale_of(s, factor);
+    }
+}
+
+// Longer rows: a workgroup per row, which it reads again for each step.
+template <typename E, int MODE>
+__global__ __launch_bounds__(1024) void row_long(RowArgs a) {
+    constexpr int T = 1024;
+    __shared__ uint64_t lds[32];
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const Row<E, MODE> r(a, (uint32_t)row);
+        float sum = 0.0f;
+        uint32_t top_bits = 0;
+        for (int c = threadIdx.x; c < a.C; c += T) {
+            const float v = r.value(c, false);
+            if (is_norm(MODE)) sum += v * v;
+            if (MODE != kNorm) top_bits = max(top_bits, __builtin_bit_cast(uint32_t, r.z32(c, v)) & 0x7FFFFFFFu);
+        }
+        float factor = 1.0f;
+        if (is_norm(MODE)) factor = 1.0f / sqrtf(over_row<T>(sum, Add(), lds, turn) / (float)a.C + a.eps);
+        Scale s = {};
+        if (MODE != kNorm) {
+            s = scale_from(over_row<T>(top_bits, Larger(), lds, turn));
+            if (!r.exact || s.tiny) {
+                const float near = s.tiny ? 0.0f : (float)s.top * kNearTop;
+                double t = 0.0;
+                for (int c = threadIdx.x; c < a.C && s.fine; c += T) {
+                    const float v = r.value(c, false);
+                    if (fabsf(r.z32(c, v)) >= near) t = Larger()(t, fabs(r.z64(c, v)));
+                }
+                t = over_row<T>(t, Larger(), lds, turn);
+                if (s.fine) s.top = t;
+            }
+            s.reach = s.top > 0.0 ? (float)(127.0 / s.top) : 0.0f;
+        }
+        int total = 0;
+        for (int c = threadIdx.x; c < a.C; c += T) {
+            const float v = r.value(c, false);
+            const float z = r.z32(c, v);
+            if (is_norm(MODE) && r.h) r.h[c] = E::from_f32(v);
             if (MODE == kNorm) {
-                static_cast<Raw *>(a.y)[b * a.y_batch + s * a.y_row + c] = E::from_f32(weight ? v * factor * E::to_f32(weight[c]) : v * factor);
+                r.y[c] = E::from_f32(z * factor);
             } else {
-                const float t = z32(c, v) * reach;
+                const float t = z * s.reach;
                 float q = rintf(t);
-                if (fine && top > 0.0 && (tiny || fabsf(t - q) > 0.5f - 0x1p-14f - fabsf(t) * 0x1p-15f)) q = (float)rint(127.0 * z64(c, v) / top);
-                const int code = fine ? (int)q : 0;
-                a.codes[b * a.c_batch + s * a.c_row + c] = (int8_t)code;
-                codes += code;
+                if (s.fine && s.top > 0.0 && (s.tiny || fabsf(t - q) > 0.5f - r.margin(t, v))) q = (float)rint(127.0 * r.z64(c, v) / s.top);
+                const int code = s.fine ? (int)q : 0;
+                r.codes[c] = (int8_t)code;
+                total += code;
             }
         }
         if (MODE != kNorm) {
             if (a.rowsum) {
-                const int total = all(codes, reinterpret_cast<int *>(lds), add);
+                total = over_row<T>(total, Add(), lds, turn);
                 if (threadIdx.x == 0) a.rowsum[row] = total;
             }
-            if (threadIdx.x == 0) a.scale[row] = !fine ? __builtin_nanf("") : top > 0.0 ? (float)(top / 127.0) * factor : 0.0f;
+            if (threadIdx.x == 0) a.scale[row] = scale_of(s, factor);
         }
     }
 }
 
+template <typename E, int MODE>
+int launch_held(const RowArgs &a, hipStream_t stream) {
+    const int pieces = (a.C + E::kVec - 1) / E::kVec;
+    const auto launch = [&](auto t, auto np) {
+        constexpr int T = decltype(t)::value, NP = decltype(np)::value, R = T < 256 ? 256 / T : 1;
+        row_held<E, MODE, T, NP><<<dim3((unsigned)std::min<int64_t>((a.rows + R - 1) / R, 1 << 20)), T < 256 ? 256 : T, 0, stream>>>(a);
+        return check_launch();
+    };
+    using std::integral_constant;
+    const auto of = [&](auto t, int np) {
+        switch (np) {
+            case 1: return launch(t, integral_constant<int, 1>());
+            case 2: return launch(t, integral_constant<int, 2>());
+            case 3: return launch(t, integral_constant<int, 3>());
+            default: return launch(t, integral_constant<int, 4>());
+        }
+    };
+    if (pieces <= 8) return launch(integral_constant<int, 8>(), integral_constant<int, 1>());
+    if (pieces <= 16) return launch(integral_constant<int, 16>(), integral_constant<int, 1>());
+    if (pieces <= 32) return launch(integral_constant<int, 32>(), integral_constant<int, 1>());
+    if (pieces <= 256) return of(integral_constant<int, 64>(), (pieces + 63) / 64);
+    if (pieces <= 1024) return of(integral_constant<int, 256>(), (pieces + 255) / 256);
+    if (pieces <= 4096) return of(integral_constant<int, 1024>(), (pieces + 1023) / 1024);
+    row_long<E, MODE><<<dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), 1024, 0, stream>>>(a);
+    return check_launch();
+}
+
 template <int MODE>
-int launch_rows(const RowArgs &a, int dtype, hipStream_t stream) {
+int launch_rows(RowArgs a, int dtype, hipStream_t stream) {
+    if (a.S > 1) {                                   // 2^(31 + l) / S rounded up, 2^l >= S
+        int l = 1;
+        while (((uint64_t)1 << l) < a.S) ++l;
+        a.S_mul = (uint32_t)((((uint64_t)1 << (31 + l)) + a.S - 1) / a.S), a.S_shift = l - 1;
+    }
     return with_type(dtype, [&](auto type) {
         using E = decltype(type);
-        row_any<E, MODE><<<dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), 256, 0, stream>>>(a);
-        return check_launch();
+        return launch_held<E, MODE>(a, stream);
     });
 }
 
@@ -174,7 +389,7 @@ int launch_quant8(const void *x, int64_t ldx, const void *up, int64_t ldu, int a
     a.codes = codes, a.scale = x_scale, a.rowsum = code_rowsum;
     a.x_row = ldx, a.s_row = ldu, a.c_row = ldc;
     a.rows = M, a.S = (uint32_t)M, a.C = (int)C, a.act = act;
-    return launch_rows<kQuant>(a, dtype, stream);
+    return act == DVDQ_ACT_NONE ? launch_rows<kQuant>(a, dtype, stream) : launch_rows<kQuantAct>(a, dtype, stream);
 }
 
 }  // namespace dvdq
