@@ -91,13 +91,15 @@ struct Row {
         if (!is_norm(MODE)) return (MODE == kQuantAct ? act64(v, act) : (double)v) * (second ? (double)E::to_f32(second[c]) : 1.0);
         return weight ? (double)v * E::to_f32(weight[c]) : (double)v;
     }
-    // How far fp32 may have 127 z / max|z| = t off.  The quotient 127 / max|z| is off by 2^-24, products by 2^-24, activations by 2^-20 of themselves
-    // and by up to 2^-15 where they fall like an exponential (see activate); v: the activation's argument.
-    __device__ __forceinline__ float margin(float t, float v) const {
+    // How far fp32 may have 127 z / max|z| = t off: the quotient 127 / max|z| by 2^-24 of t, products by 2^-24, activations by 2^-15 of themselves
+    // where they fall like an exponential (see activate).
+    __device__ __forceinline__ float margin(float t) const {
         if (MODE != kQuantAct) return exact ? 0x1p-16f : 0x1p-15f;
-        return 0x1p-15f + fabsf(t) * (v < -2.0f ? 0x1p-15f : 0x1p-18f);
+        return 0x1p-15f + fabsf(t) * 0x1p-15f;
     }
 };
+// An activation is good to 2^-18 of itself up to where it has fallen to 7.5e-5 (e^-12 times an argument of 12; see activate); beyond, it is that small.
+constexpr float kGood = 0x1p-18f, kFallen = 7.5e-5f;
 constexpr float kTiny = 0x1p-60f;                    // below, products in fp32 may have lost digits
 constexpr float kNearTop = 1.0f - 0x1p-13f;          // what may turn out to be the largest, as a share of the largest in fp32
 
@@ -146,6 +148,65 @@ static __device__ __forceinline__ Scale scale_from(uint32_t top_bits) {
     return {(double)top, 0.0f, top_bits < 0x7F800000u, top < kTiny};
 }
 
+// 16 bytes of a row as four words, which stay four registers also where the piece across a row's end is put together by element (as an array of
+// elements that was 8: 92 registers for three pieces of the norm in place of 70).
+template <typename E>
+static __device__ __forceinline__ uint4 load_words(const typename E::Raw *p, int n) {
+    constexpr int V = E::kVec;
+    if (n >= V) return __builtin_bit_cast(uint4, *reinterpret_cast<const Piece<E> *>(p));
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (e < n) {
+            if constexpr (V == 8) w[e / 2] |= (uint32_t)p[e] << 16 * (e % 2);
+            else w[e] = __builtin_bit_cast(uint32_t, p[e]);
+        }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+static __device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+template <typename E>
+static __device__ __forceinline__ float element(const uint4 &v, int e) {
+    if constexpr (E::kVec == 8) return E::to_f32((uint16_t)(word_of(v, e / 2) >> 16 * (e % 2)));
+    else return __builtin_bit_cast(float, word_of(v, e));
+}
+template <typename E>
+static __device__ __forceinline__ uint4 rounded(const float (&v)[E::kVec]) {
+    if constexpr (E::kVec == 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = E::from_f32(v[2 * i]) | (uint32_t)E::from_f32(v[2 * i + 1]) << 16;
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        return __builtin_bit_cast(uint4, v);
+    }
+}
+template <typename E>
+static __device__ __forceinline__ void store_words(typename E::Raw *p, const uint4 &v, int n) {
+    constexpr int V = E::kVec;
+    if (n >= V) {
+        *reinterpret_cast<Piece<E> *>(p) = __builtin_bit_cast(Piece<E>, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        if (e < n) {
+            if constexpr (V == 8) p[e] = (uint16_t)(word_of(v, e / 2) >> 16 * (e % 2));
+            else p[e] = element<E>(v, e);
+        }
+}
+
+// the larger of |a|, |b| and c; NaN if one of them is
+static __device__ __forceinline__ float maximum3(float a, float b, float c) {
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(a), fabsf(b)), c);
+}
+template <typename E, int ACT, int NP, int V>
+static __device__ __forceinline__ void activate_all(float (&z)[NP][V], const uint4 (&x)[NP]) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int e = 0; e < V; ++e) z[i][e] = activate<ACT>(element<E>(x[i], e));
+}
+
 // T threads a row, which they hold: NP pieces of 16 bytes each.
 template <typename E, int MODE, int T, int NP>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
@@ -159,43 +220,56 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
         uint32_t row = (uint32_t)(there ? mine : a.rows - 1);
         if (T >= 64) row = __builtin_amdgcn_readfirstlane(row);
         const Row<E, MODE> r(a, row);
-        Piece<E> px[NP], ps[NP], pw[NP];
+        uint4 px[NP], ps[NP], pw[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int c = (l + T * i) * V, n = a.C - c;
-            px[i] = load_piece<E>(r.x + c, n);
-            if (r.second) ps[i] = load_piece<E>(r.second + c, n);
-            if (is_norm(MODE) && r.weight) pw[i] = load_piece<E>(r.weight + c, n);
+            px[i] = load_words<E>(r.x + c, n);
+            if (r.second) ps[i] = load_words<E>(r.second + c, n);
+            if (is_norm(MODE) && r.weight) pw[i] = load_words<E>(r.weight + c, n);
         }
-        float z[NP][V], sum = 0.0f;
-        uint32_t top_bits = 0;
+        float z[NP][V], sum = 0.0f, top = 0.0f, up_top = 0.0f;
+        if constexpr (MODE == kQuantAct) {
+            switch (a.act) {
+                case DVDQ_ACT_SILU: activate_all<E, DVDQ_ACT_SILU>(z, px); break;
+                case DVDQ_ACT_GELU_TANH: activate_all<E, DVDQ_ACT_GELU_TANH>(z, px); break;
+                default: activate_all<E, DVDQ_ACT_GELU>(z, px);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int c = (l + T * i) * V, n = a.C - c;
-            if (!is_norm(MODE)) {
-#pragma unroll
-                for (int e = 0; e < V; ++e) z[i][e] = MODE == kQuantAct ? act32(E::to_f32(px[i].e[e]), r.act) : E::to_f32(px[i].e[e]);
-                if (r.second)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) z[i][e] *= E::to_f32(ps[i].e[e]);
-            } else {
+            if (is_norm(MODE)) {
                 if (r.second) {
+                    float v[V];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) px[i].e[e] = E::from_f32(E::to_f32(px[i].e[e]) + E::to_f32(ps[i].e[e]));
-                    if (there) store_piece<E>(r.h + c, px[i], n);
+                    for (int e = 0; e < V; ++e) v[e] = element<E>(px[i], e) + element<E>(ps[i], e);
+                    px[i] = rounded<E>(v);
+                    if (there) store_words<E>(r.h + c, px[i], n);
                 }
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    z[i][e] = E::to_f32(px[i].e[e]);
-                    sum += z[i][e] * z[i][e];
+                    z[i][e] = element<E>(px[i], e);
+                    sum = fmaf(z[i][e], z[i][e], sum);
                 }
                 if (r.weight)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) z[i][e] *= E::to_f32(pw[i].e[e]);
+                    for (int e = 0; e < V; ++e) z[i][e] *= element<E>(pw[i], e);
+            } else {
+                if (MODE == kQuant)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) z[i][e] = element<E>(px[i], e);
+                if (r.second)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float up = element<E>(ps[i], e);
+                        if (MODE == kQuantAct) up_top = fmaxf(up_top, fabsf(up));
+                        z[i][e] *= up;
+                    }
             }
             if (MODE != kNorm)
 #pragma unroll
-                for (int e = 0; e < V; ++e) top_bits = max(top_bits, __builtin_bit_cast(uint32_t, z[i][e]) & 0x7FFFFFFFu);   // (a NaN is above infinity)
+                for (int e = 0; e < V; e += 2) top = maximum3(z[i][e], z[i][e + 1], top);
         }
         float factor = 1.0f;
         if (is_norm(MODE)) factor = 1.0f / sqrtf(over_row<T>(sum, Add(), lds, turn) / (float)a.C + a.eps);
@@ -203,28 +277,33 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 const int c = (l + T * i) * V, n = a.C - c;
-                Piece<E> o;
+                float v[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) o.e[e] = E::from_f32(z[i][e] * factor);
-                if (there) store_piece<E>(r.y + c, o, n);
+                for (int e = 0; e < V; ++e) v[e] = z[i][e] * factor;
+                if (there) store_words<E>(r.y + c, rounded<E>(v), n);
             }
             continue;
         }
         // Which of a thread's elements need a second look: bit V i + e.  That goes by the values in memory, so that there is one place for it.
-        static_assert(NP * V <= 32, "a bit each");
-        const auto place = [&](uint32_t bit) { return (l + T * (int)(bit / V)) * V + (int)(bit % V); };
-        Scale s = scale_from(over_row<T>(top_bits, Larger(), lds, turn));
+        static_assert(NP * V <= 64, "a bit each");
+        using Mask = std::conditional_t<NP * V <= 32, uint32_t, uint64_t>;
+        const auto place = [&](Mask which) {
+            const int bit = sizeof(Mask) == 4 ? __builtin_ctz((uint32_t)which) : __builtin_ctzll(which);
+            return (l + T * (bit / V)) * V + bit % V;
+        };
+        Scale s = scale_from(over_row<T>(__builtin_bit_cast(uint32_t, top) & 0x7FFFFFFFu, Larger(), lds, turn));   // (a NaN's bits are above infinity's)
         if (!r.exact || s.tiny) {
             double t = 0.0;
             if (s.fine) {
                 const float near = s.tiny ? 0.0f : (float)s.top * kNearTop;
-                uint32_t which = 0;
+                Mask which = 0;
+                if (top >= near)
 #pragma unroll
-                for (int i = 0; i < NP; ++i)
+                    for (int i = 0; i < NP; ++i)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) which |= (fabsf(z[i][e]) >= near ? 1u : 0u) << (V * i + e);
+                        for (int e = 0; e < V; ++e) which |= (Mask)(fabsf(z[i][e]) >= near ? 1 : 0) << (V * i + e);
                 for (; which; which &= which - 1) {
-                    const int c = place(__builtin_ctz(which));
+                    const int c = place(which);
                     if (c < a.C) t = Larger()(t, fabs(r.z64(c, r.value(c, true))));
                 }
             }
@@ -233,28 +312,45 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
         }
         s.reach = s.top > 0.0 ? (float)(127.0 / s.top) : 0.0f;
         int total = 0;
-        uint32_t near = 0;
+        float far = 0.0f;                            // the furthest that t is from a whole number
+        constexpr float kMagic = 12582912.0f;        // 1.5 2^23: t + that has the whole number next to t in its lowest bits
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int c = (l + T * i) * V, n = a.C - c;
-            // t + 1.5 2^23 has the whole number next to t in its lowest bits
-            constexpr float kMagic = 12582912.0f;
-            Piece<Code, V> o;
-            int word[V / 4];
+            uint32_t m[V], word[V / 4];
+            float off[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float m = fmaf(z[i][e], s.reach, kMagic), q = m - kMagic, off = fmaf(z[i][e], s.reach, -q);
-                near |= (fabsf(off) > 0.5f - r.margin(q, MODE == kQuantAct ? E::to_f32(px[i].e[e]) : 0.0f) ? 1u : 0u) << (V * i + e);
-                o.e[e] = s.fine ? (int8_t)__builtin_bit_cast(uint32_t, m) : 0;
+                const float t = fmaf(z[i][e], s.reach, kMagic), q = t - kMagic;
+                m[e] = __builtin_bit_cast(uint32_t, t);
+                off[e] = fabsf(fmaf(z[i][e], s.reach, -q));
+                if (MODE == kQuantAct) off[e] = fmaf(fabsf(q), kGood, off[e]);
             }
-            if (there) store_piece<Code, V>(r.codes + c, o, n);
-            __builtin_memcpy(word, &o, V);
 #pragma unroll
-            for (int w = 0; w < V / 4; ++w) total = __builtin_amdgcn_sdot4(word[w], 0x01010101, total, false);
+            for (int e = 0; e < V; e += 2) far = maximum3(off[e], off[e + 1], far);
+#pragma unroll
+            for (int w = 0; w < V / 4; ++w) {
+                word[w] = __builtin_amdgcn_perm(m[4 * w + 1], m[4 * w], 0x0C0C0400u) | __builtin_amdgcn_perm(m[4 * w + 3], m[4 * w + 2], 0x04000C0Cu);
+                if (!s.fine) word[w] = 0;
+                if (a.rowsum) total = __builtin_amdgcn_sdot4((int)word[w], 0x01010101, total, false);
+            }
+            Piece<Code, V> o;
+            __builtin_memcpy(&o, word, V);
+            if (there) store_piece<Code, V>(r.codes + c, o, n);
         }
-        if (s.fine && s.top > 0.0)
-            for (near = s.tiny ? ~0u >> (32 - NP * V) : near; near; near &= near - 1) {
-                const int c = place(__builtin_ctz(near));
+        // (a part that is not there is z = 0)
+        const bool fallen = MODE == kQuantAct && (r.second ? up_top : 1.0f) * kFallen * s.reach > 0.25f;
+        if (s.fine && s.top > 0.0 && (s.tiny || fallen || far > 0.5f - (r.exact ? 0x1p-16f : 0x1p-15f))) {
+            Mask near = 0;
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float t = z[i][e] * s.reach;
+                    near |= (Mask)(s.tiny || fabsf(t - rintf(t)) > 0.5f - r.margin(t) ? 1 : 0) << (V * i + e);
+                }
+            for (; near; near &= near - 1) {
+                const int c = place(near);
                 if (c >= a.C) break;
                 const int code = (int)rint(127.0 * r.z64(c, r.value(c, true)) / s.top);
                 if (there) {
@@ -262,6 +358,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
                     r.codes[c] = (int8_t)code;
                 }
             }
+        }
         if (a.rowsum) {
             total = over_row<T>(total, Add(), lds, turn);
             if (l == 0 && there) a.rowsum[row] = total;
@@ -312,7 +409,7 @@ __global__ __launch_bounds__(1024) void row_long(RowArgs a) {
             } else {
                 const float t = z * s.reach;
                 float q = rintf(t);
-                if (s.fine && s.top > 0.0 && (s.tiny || fabsf(t - q) > 0.5f - r.margin(t, v))) q = (float)rint(127.0 * r.z64(c, v) / s.top);
+                if (s.fine && s.top > 0.0 && (s.tiny || fabsf(t - q) > 0.5f - r.margin(t))) q = (float)rint(127.0 * r.z64(c, v) / s.top);
                 const int code = s.fine ? (int)q : 0;
                 r.codes[c] = (int8_t)code;
                 total += code;
@@ -337,20 +434,22 @@ int launch_held(const RowArgs &a, hipStream_t stream) {
         return check_launch();
     };
     using std::integral_constant;
-    const auto of = [&](auto t, int np) {
-        switch (np) {
-            case 1: return launch(t, integral_constant<int, 1>());
-            case 2: return launch(t, integral_constant<int, 2>());
-            case 3: return launch(t, integral_constant<int, 3>());
-            default: return launch(t, integral_constant<int, 4>());
-        }
-    };
     if (pieces <= 8) return launch(integral_constant<int, 8>(), integral_constant<int, 1>());
     if (pieces <= 16) return launch(integral_constant<int, 16>(), integral_constant<int, 1>());
     if (pieces <= 32) return launch(integral_constant<int, 32>(), integral_constant<int, 1>());
-    if (pieces <= 256) return of(integral_constant<int, 64>(), (pieces + 63) / 64);
-    if (pieces <= 1024) return of(integral_constant<int, 256>(), (pieces + 255) / 256);
-    if (pieces <= 4096) return of(integral_constant<int, 1024>(), (pieces + 1023) / 1024);
+    const integral_constant<int, 64> wave;
+    if (pieces <= 64) return launch(wave, integral_constant<int, 1>());
+    if (pieces <= 128) return launch(wave, integral_constant<int, 2>());
+    if (pieces <= 192) return launch(wave, integral_constant<int, 3>());
+    if (pieces <= 256) return launch(wave, integral_constant<int, 4>());
+    const integral_constant<int, 256> four;
+    if (pieces <= 512) return launch(four, integral_constant<int, 2>());
+    if (pieces <= 768) return launch(four, integral_constant<int, 3>());
+    if (pieces <= 1024) return launch(four, integral_constant<int, 4>());
+    if (pieces <= 1280) return launch(four, integral_constant<int, 5>());
+    if (pieces <= 1536) return launch(four, integral_constant<int, 6>());
+    if (pieces <= 2048) return launch(four, integral_constant<int, 8>());
+    if (pieces <= 4096) return launch(integral_constant<int, 1024>(), integral_constant<int, 4>());
     row_long<E, MODE><<<dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), 1024, 0, stream>>>(a);
     return check_launch();
 }
