@@ -24,10 +24,10 @@ struct RowArgs {
     float *scale;
     int32_t *rowsum;
     int64_t x_batch, x_row, s_batch, s_row, h_batch, h_row, y_batch, y_row, c_batch, c_row;
-    int64_t rows;
+    int64_t first, rows;                             // of this launch's rows; all rows
     uint32_t S, S_mul, S_shift;                      // rows of a batch; row / S = row * S_mul >> 32 + S_shift for rows below 2^31 (S > 1)
     int C, act;
-    float eps;
+    float eps, share;                                // share: 1 / C
 };
 
 struct Code {
@@ -91,7 +91,7 @@ struct Row {
         if (!is_norm(MODE)) return (MODE == kQuantAct ? act64(v, act) : (double)v) * (second ? (double)E::to_f32(second[c]) : 1.0);
         return weight ? (double)v * E::to_f32(weight[c]) : (double)v;
     }
-    // How far fp32 may have 127 z / max|z| = t off: the quotient 127 / max|z| by 2^-24 of t, products by 2^-24, activations by 2^-15 of themselves
+    // How far fp32 may have 127 z / max|z| = t off: the quotient 127 / max|z| by 2^-24 of t (twice that where the maximum is not an fp32 number), products by 2^-24, activations by 2^-15 of themselves
     // where they fall like an exponential (see activate).
     __device__ __forceinline__ float margin(float t) const {
         if (MODE != kQuantAct) return exact ? 0x1p-16f : 0x1p-15f;
@@ -141,7 +141,7 @@ struct Scale {
     bool fine, tiny; // no NaN or infinity; products may have lost digits
 };
 static __device__ __forceinline__ float scale_of(const Scale &s, float factor) {
-    return !s.fine ? __builtin_nanf("") : s.top > 0.0 ? (float)(s.top / 127.0) * factor : 0.0f;
+    return !s.fine ? __builtin_nanf("") : s.top > 0.0 ? (float)s.top * (1.0f / 127.0f) * factor : 0.0f;
 }
 static __device__ __forceinline__ Scale scale_from(uint32_t top_bits) {
     const float top = __builtin_bit_cast(float, top_bits);
@@ -211,160 +211,160 @@ static __device__ __forceinline__ void activate_all(float (&z)[NP][V], const uin
 template <typename E, int MODE, int T, int NP>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
     constexpr int V = E::kVec, R = T < 256 ? 256 / T : 1;
+    // the row's end lies in a thread's last piece, or where not every number of pieces has a kernel, in its last two
+    constexpr int kWhole = T == 64 || (T == 256 && NP < 8) ? NP - 1 : std::max(NP - 2, 0);
     __shared__ uint64_t lds[32];
     int turn = 0;
     const int l = threadIdx.x % T;
-    for (int64_t row0 = (int64_t)blockIdx.x * R; row0 < a.rows; row0 += (int64_t)gridDim.x * R) {
-        const int64_t mine = row0 + threadIdx.x / T;
-        const bool there = R == 1 || mine < a.rows;
-        uint32_t row = (uint32_t)(there ? mine : a.rows - 1);
-        if (T >= 64) row = __builtin_amdgcn_readfirstlane(row);
-        const Row<E, MODE> r(a, row);
-        uint4 px[NP], ps[NP], pw[NP];
+    const int64_t mine = a.first + (int64_t)blockIdx.x * R + threadIdx.x / T;
+    const bool there = R == 1 || mine < a.rows;
+    uint32_t row = (uint32_t)(there ? mine : a.rows - 1);
+    if (T >= 64) row = __builtin_amdgcn_readfirstlane(row);
+    const Row<E, MODE> r(a, row);
+    uint4 px[NP], ps[NP], pw[NP];
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int c = (l + T * i) * V, n = a.C - c;
-            px[i] = load_words<E>(r.x + c, n);
-            if (r.second) ps[i] = load_words<E>(r.second + c, n);
-            if (is_norm(MODE) && r.weight) pw[i] = load_words<E>(r.weight + c, n);
+    for (int i = 0; i < NP; ++i) {
+        const int c = (l + T * i) * V, n = i < kWhole ? V : a.C - c;
+        px[i] = load_words<E>(r.x + c, n);
+        if (r.second) ps[i] = load_words<E>(r.second + c, n);
+        if (is_norm(MODE) && r.weight) pw[i] = load_words<E>(r.weight + c, n);
+    }
+    float z[NP][V], sum = 0.0f, top = 0.0f, up_top = 0.0f;
+    if constexpr (MODE == kQuantAct) {
+        switch (a.act) {
+            case DVDQ_ACT_SILU: activate_all<E, DVDQ_ACT_SILU>(z, px); break;
+            case DVDQ_ACT_GELU_TANH: activate_all<E, DVDQ_ACT_GELU_TANH>(z, px); break;
+            default: activate_all<E, DVDQ_ACT_GELU>(z, px);
         }
-        float z[NP][V], sum = 0.0f, top = 0.0f, up_top = 0.0f;
-        if constexpr (MODE == kQuantAct) {
-            switch (a.act) {
-                case DVDQ_ACT_SILU: activate_all<E, DVDQ_ACT_SILU>(z, px); break;
-                case DVDQ_ACT_GELU_TANH: activate_all<E, DVDQ_ACT_GELU_TANH>(z, px); break;
-                default: activate_all<E, DVDQ_ACT_GELU>(z, px);
-            }
-        }
+    }
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int c = (l + T * i) * V, n = a.C - c;
-            if (is_norm(MODE)) {
-                if (r.second) {
-                    float v[V];
-#pragma unroll
-                    for (int e = 0; e < V; ++e) v[e] = element<E>(px[i], e) + element<E>(ps[i], e);
-                    px[i] = rounded<E>(v);
-                    if (there) store_words<E>(r.h + c, px[i], n);
-                }
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    z[i][e] = element<E>(px[i], e);
-                    sum = fmaf(z[i][e], z[i][e], sum);
-                }
-                if (r.weight)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) z[i][e] *= element<E>(pw[i], e);
-            } else {
-                if (MODE == kQuant)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) z[i][e] = element<E>(px[i], e);
-                if (r.second)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float up = element<E>(ps[i], e);
-                        if (MODE == kQuantAct) up_top = fmaxf(up_top, fabsf(up));
-                        z[i][e] *= up;
-                    }
-            }
-            if (MODE != kNorm)
-#pragma unroll
-                for (int e = 0; e < V; e += 2) top = maximum3(z[i][e], z[i][e + 1], top);
-        }
-        float factor = 1.0f;
-        if (is_norm(MODE)) factor = 1.0f / sqrtf(over_row<T>(sum, Add(), lds, turn) / (float)a.C + a.eps);
-        if (MODE == kNorm) {
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const int c = (l + T * i) * V, n = a.C - c;
+    for (int i = 0; i < NP; ++i) {
+        const int c = (l + T * i) * V, n = i < kWhole ? V : a.C - c;
+        if (is_norm(MODE)) {
+            if (r.second) {
                 float v[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) v[e] = z[i][e] * factor;
-                if (there) store_words<E>(r.y + c, rounded<E>(v), n);
+                for (int e = 0; e < V; ++e) v[e] = element<E>(px[i], e) + element<E>(ps[i], e);
+                px[i] = rounded<E>(v);
+                if (there) store_words<E>(r.h + c, px[i], n);
             }
-            continue;
-        }
-        // Which of a thread's elements need a second look: bit V i + e.  That goes by the values in memory, so that there is one place for it.
-        static_assert(NP * V <= 64, "a bit each");
-        using Mask = std::conditional_t<NP * V <= 32, uint32_t, uint64_t>;
-        const auto place = [&](Mask which) {
-            const int bit = sizeof(Mask) == 4 ? __builtin_ctz((uint32_t)which) : __builtin_ctzll(which);
-            return (l + T * (bit / V)) * V + bit % V;
-        };
-        Scale s = scale_from(over_row<T>(__builtin_bit_cast(uint32_t, top) & 0x7FFFFFFFu, Larger(), lds, turn));   // (a NaN's bits are above infinity's)
-        if (!r.exact || s.tiny) {
-            double t = 0.0;
-            if (s.fine) {
-                const float near = s.tiny ? 0.0f : (float)s.top * kNearTop;
-                Mask which = 0;
-                if (top >= near)
-#pragma unroll
-                    for (int i = 0; i < NP; ++i)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) which |= (Mask)(fabsf(z[i][e]) >= near ? 1 : 0) << (V * i + e);
-                for (; which; which &= which - 1) {
-                    const int c = place(which);
-                    if (c < a.C) t = Larger()(t, fabs(r.z64(c, r.value(c, true))));
-                }
-            }
-            t = over_row<T>(t, Larger(), lds, turn);
-            if (s.fine) s.top = t;
-        }
-        s.reach = s.top > 0.0 ? (float)(127.0 / s.top) : 0.0f;
-        int total = 0;
-        float far = 0.0f;                            // the furthest that t is from a whole number
-        constexpr float kMagic = 12582912.0f;        // 1.5 2^23: t + that has the whole number next to t in its lowest bits
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int c = (l + T * i) * V, n = a.C - c;
-            uint32_t m[V], word[V / 4];
-            float off[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float t = fmaf(z[i][e], s.reach, kMagic), q = t - kMagic;
-                m[e] = __builtin_bit_cast(uint32_t, t);
-                off[e] = fabsf(fmaf(z[i][e], s.reach, -q));
-                if (MODE == kQuantAct) off[e] = fmaf(fabsf(q), kGood, off[e]);
+                z[i][e] = element<E>(px[i], e);
+                sum = fmaf(z[i][e], z[i][e], sum);
             }
+            if (r.weight)
 #pragma unroll
-            for (int e = 0; e < V; e += 2) far = maximum3(off[e], off[e + 1], far);
+                for (int e = 0; e < V; ++e) z[i][e] *= element<E>(pw[i], e);
+        } else {
+            if (MODE == kQuant)
 #pragma unroll
-            for (int w = 0; w < V / 4; ++w) {
-                word[w] = __builtin_amdgcn_perm(m[4 * w + 1], m[4 * w], 0x0C0C0400u) | __builtin_amdgcn_perm(m[4 * w + 3], m[4 * w + 2], 0x04000C0Cu);
-                if (!s.fine) word[w] = 0;
-                if (a.rowsum) total = __builtin_amdgcn_sdot4((int)word[w], 0x01010101, total, false);
-            }
-            Piece<Code, V> o;
-            __builtin_memcpy(&o, word, V);
-            if (there) store_piece<Code, V>(r.codes + c, o, n);
-        }
-        // (a part that is not there is z = 0)
-        const bool fallen = MODE == kQuantAct && (r.second ? up_top : 1.0f) * kFallen * s.reach > 0.25f;
-        if (s.fine && s.top > 0.0 && (s.tiny || fallen || far > 0.5f - (r.exact ? 0x1p-16f : 0x1p-15f))) {
-            Mask near = 0;
-#pragma unroll
-            for (int i = 0; i < NP; ++i)
+                for (int e = 0; e < V; ++e) z[i][e] = element<E>(px[i], e);
+            if (r.second)
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float t = z[i][e] * s.reach;
-                    near |= (Mask)(s.tiny || fabsf(t - rintf(t)) > 0.5f - r.margin(t) ? 1 : 0) << (V * i + e);
+                    const float up = element<E>(ps[i], e);
+                    if (MODE == kQuantAct) up_top = fmaxf(up_top, fabsf(up));
+                    z[i][e] *= up;
                 }
-            for (; near; near &= near - 1) {
-                const int c = place(near);
-                if (c >= a.C) break;
-                const int code = (int)rint(127.0 * r.z64(c, r.value(c, true)) / s.top);
-                if (there) {
-                    total += code - r.codes[c];
-                    r.codes[c] = (int8_t)code;
-                }
+        }
+        if (MODE != kNorm)
+#pragma unroll
+            for (int e = 0; e < V; e += 2) top = maximum3(z[i][e], z[i][e + 1], top);
+    }
+    float factor = 1.0f;
+    if (is_norm(MODE)) factor = rsqrtf(fmaf(over_row<T>(sum, Add(), lds, turn), a.share, a.eps));
+    if (MODE == kNorm) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int c = (l + T * i) * V, n = i < kWhole ? V : a.C - c;
+            float v[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = z[i][e] * factor;
+            if (there) store_words<E>(r.y + c, rounded<E>(v), n);
+        }
+        return;
+    }
+    // Which of a thread's elements need a second look: bit V i + e.  That goes by the values in memory, so that there is one place for it.
+    static_assert(NP * V <= 64, "a bit each");
+    using Mask = std::conditional_t<NP * V <= 32, uint32_t, uint64_t>;
+    const auto place = [&](Mask which) {
+        const int bit = sizeof(Mask) == 4 ? __builtin_ctz((uint32_t)which) : __builtin_ctzll(which);
+        return (l + T * (bit / V)) * V + bit % V;
+    };
+    Scale s = scale_from(over_row<T>(__builtin_bit_cast(uint32_t, top) & 0x7FFFFFFFu, Larger(), lds, turn));   // (a NaN's bits are above infinity's)
+    if (!r.exact || s.tiny) {
+        double t = 0.0;
+        if (s.fine) {
+            const float near = s.tiny ? 0.0f : (float)s.top * kNearTop;
+            Mask which = 0;
+            if (top >= near)
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) which |= (Mask)(fabsf(z[i][e]) >= near ? 1 : 0) << (V * i + e);
+            for (; which; which &= which - 1) {
+                const int c = place(which);
+                if (c < a.C) t = Larger()(t, fabs(r.z64(c, r.value(c, true))));
             }
         }
-        if (a.rowsum) {
-            total = over_row<T>(total, Add(), lds, turn);
-            if (l == 0 && there) a.rowsum[row] = total;
-        }
-        if (l == 0 && there) a.scale[row] = scale_of(s, factor);
+        t = over_row<T>(t, Larger(), lds, turn);
+        if (s.fine) s.top = t;
     }
+    s.reach = s.top > 0.0 ? 127.0f / (float)s.top : 0.0f;
+    int total = 0;
+    float far = 0.0f;                            // the furthest that t is from a whole number
+    constexpr float kMagic = 12582912.0f;        // 1.5 2^23: t + that has the whole number next to t in its lowest bits
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int c = (l + T * i) * V, n = i < kWhole ? V : a.C - c;
+        uint32_t m[V], word[V / 4];
+        float off[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float t = fmaf(z[i][e], s.reach, kMagic), q = t - kMagic;
+            m[e] = __builtin_bit_cast(uint32_t, t);
+            off[e] = fabsf(fmaf(z[i][e], s.reach, -q));
+            if (MODE == kQuantAct) off[e] = fmaf(fabsf(q), kGood, off[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < V; e += 2) far = maximum3(off[e], off[e + 1], far);
+#pragma unroll
+        for (int w = 0; w < V / 4; ++w) {
+            word[w] = __builtin_amdgcn_perm(m[4 * w + 1], m[4 * w], 0x0C0C0400u) | __builtin_amdgcn_perm(m[4 * w + 3], m[4 * w + 2], 0x04000C0Cu);
+            if (!s.fine) word[w] = 0;
+            if (a.rowsum) total = __builtin_amdgcn_sdot4((int)word[w], 0x01010101, total, false);
+        }
+        Piece<Code, V> o;
+        __builtin_memcpy(&o, word, V);
+        if (there) store_piece<Code, V>(r.codes + c, o, n);
+    }
+    // (a part that is not there is z = 0)
+    const bool fallen = MODE == kQuantAct && (r.second ? up_top : 1.0f) * kFallen * s.reach > 0.25f;
+    if (s.fine && s.top > 0.0 && (s.tiny || fallen || far > 0.5f - (r.exact ? 0x1p-16f : 0x1p-15f))) {
+        Mask near = 0;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float t = z[i][e] * s.reach;
+                near |= (Mask)(s.tiny || fabsf(t - rintf(t)) > 0.5f - r.margin(t) ? 1 : 0) << (V * i + e);
+            }
+        for (; near; near &= near - 1) {
+            const int c = place(near);
+            if (c >= a.C) break;
+            const int code = (int)rint(127.0 * r.z64(c, r.value(c, true)) / s.top);
+            if (there) {
+                total += code - r.codes[c];
+                r.codes[c] = (int8_t)code;
+            }
+        }
+    }
+    if (a.rowsum) {
+        total = over_row<T>(total, Add(), lds, turn);
+        if (l == 0 && there) a.rowsum[row] = total;
+    }
+    if (l == 0 && there) a.scale[row] = scale_of(s, factor);
 }
 
 // Longer rows: a workgroup per row, which it reads again for each step.
@@ -383,7 +383,7 @@ __global__ __launch_bounds__(1024) void row_long(RowArgs a) {
             if (MODE != kNorm) top_bits = max(top_bits, __builtin_bit_cast(uint32_t, r.z32(c, v)) & 0x7FFFFFFFu);
         }
         float factor = 1.0f;
-        if (is_norm(MODE)) factor = 1.0f / sqrtf(over_row<T>(sum, Add(), lds, turn) / (float)a.C + a.eps);
+        if (is_norm(MODE)) factor = rsqrtf(fmaf(over_row<T>(sum, Add(), lds, turn), a.share, a.eps));
         Scale s = {};
         if (MODE != kNorm) {
             s = scale_from(over_row<T>(top_bits, Larger(), lds, turn));
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(1024) void row_long(RowArgs a) {
                 t = over_row<T>(t, Larger(), lds, turn);
                 if (s.fine) s.top = t;
             }
-            s.reach = s.top > 0.0 ? (float)(127.0 / s.top) : 0.0f;
+            s.reach = s.top > 0.0 ? 127.0f / (float)s.top : 0.0f;
         }
         int total = 0;
         for (int c = threadIdx.x; c < a.C; c += T) {
@@ -430,8 +430,14 @@ int launch_held(const RowArgs &a, hipStream_t stream) {
     const int pieces = (a.C + E::kVec - 1) / E::kVec;
     const auto launch = [&](auto t, auto np) {
         constexpr int T = decltype(t)::value, NP = decltype(np)::value, R = T < 256 ? 256 / T : 1;
-        row_held<E, MODE, T, NP><<<dim3((unsigned)std::min<int64_t>((a.rows + R - 1) / R, 1 << 20)), T < 256 ? 256 : T, 0, stream>>>(a);
-        return check_launch();
+        // (a launch has less than 2^32 threads; a loop in the kernel instead costs it 20 registers of constants)
+        for (RowArgs part = a; part.first < a.rows; part.first += (int64_t)R << 21) {
+            const int64_t workgroups = std::min<int64_t>((a.rows - part.first + R - 1) / R, 1 << 21);
+            row_held<E, MODE, T, NP><<<dim3((unsigned)workgroups), T < 256 ? 256 : T, 0, stream>>>(part);
+            const int rc = check_launch();
+            if (rc != DVDQ_OK) return rc;
+        }
+        return (int)DVDQ_OK;
     };
     using std::integral_constant;
     if (pieces <= 8) return launch(integral_constant<int, 8>(), integral_constant<int, 1>());
@@ -477,7 +483,7 @@ int launch_rms_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_ba
     a.codes = codes, a.scale = x_scale, a.rowsum = code_rowsum;
     a.x_batch = x_batch, a.x_row = x_row, a.s_batch = r_batch, a.s_row = r_row, a.h_batch = h_batch, a.h_row = h_row;
     a.y_batch = y_batch, a.y_row = y_row, a.c_batch = c_batch, a.c_row = c_row;
-    a.rows = B * S, a.S = (uint32_t)S, a.C = (int)C, a.eps = eps;
+    a.rows = B * S, a.S = (uint32_t)S, a.C = (int)C, a.eps = eps, a.share = 1.0f / (float)C;
     return y ? launch_rows<kNorm>(a, dtype, stream) : launch_rows<kNormCodes>(a, dtype, stream);
 }
 
