@@ -440,6 +440,9 @@ int launch_held(const RowArgs &a, hipStream_t stream) {
         return (int)DVDQ_OK;
     };
     using std::integral_constant;
+    // As few threads as hold the row in registers, up to 8 pieces each: no exchange through LDS up to 256 pieces, and more rows at once on a
+    // compute unit.  32760 x 8960 bf16 with 256 threads of 5 pieces against 512 of 3, us: norm 203 and 199, its codes 163 and 216, quant8 179 and 188,
+    // gated 323 and 424; 32760 x 13824 fp32 with 512 threads of 8 against 1024 of 4: 617 and 622, 509 and 669, 392 and 390, 835 and 915.
     if (pieces <= 8) return launch(integral_constant<int, 8>(), integral_constant<int, 1>());
     if (pieces <= 16) return launch(integral_constant<int, 16>(), integral_constant<int, 1>());
     if (pieces <= 32) return launch(integral_constant<int, 32>(), integral_constant<int, 1>());
@@ -455,7 +458,9 @@ int launch_held(const RowArgs &a, hipStream_t stream) {
     if (pieces <= 1280) return launch(four, integral_constant<int, 5>());
     if (pieces <= 1536) return launch(four, integral_constant<int, 6>());
     if (pieces <= 2048) return launch(four, integral_constant<int, 8>());
-    if (pieces <= 4096) return launch(integral_constant<int, 1024>(), integral_constant<int, 4>());
+    const integral_constant<int, 512> eight;
+    if (pieces <= 3072) return launch(eight, integral_constant<int, 6>());
+    if (pieces <= 4096) return launch(eight, integral_constant<int, 8>());
     row_long<E, MODE><<<dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), 1024, 0, stream>>>(a);
     return check_launch();
 }
