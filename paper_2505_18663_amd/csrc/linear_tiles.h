@@ -69,21 +69,68 @@ struct LinearArgs {
 };
 constexpr int kPart = 4;               // in the place of an activation: leave the sums of a part of K for linear_join
 
+// Eight elements as words, which stay so many registers where a branch or a row's end puts them together (as an array of elements each would have
+// a register of its own).
+template <typename E>
+struct Eight {
+    static constexpr int kWords = sizeof(typename E::Raw);   // twice that many words
+    uint32_t w[2 * kWords];
+    __device__ __forceinline__ float at(int i) const {
+        if constexpr (kWords == 2) return E::to_f32((uint16_t)(w[i / 2] >> 16 * (i % 2)));
+        else return __builtin_bit_cast(float, w[i]);
+    }
+    static __device__ __forceinline__ Eight load(const typename E::Raw *p, int n) {
+        if (n >= 8) return __builtin_bit_cast(Eight, *reinterpret_cast<const Piece<E, 8> *>(p));
+        Eight r = {};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) {
+                if constexpr (kWords == 2) r.w[i / 2] |= (uint32_t)p[i] << 16 * (i % 2);
+                else r.w[i] = __builtin_bit_cast(uint32_t, p[i]);
+            }
+        return r;
+    }
+    static __device__ __forceinline__ Eight rounded(const float (&v)[8]) {
+        Eight r;
+#pragma unroll
+        for (int i = 0; i < 2 * kWords; ++i) {
+            if constexpr (kWords == 2) r.w[i] = E::from_f32(v[2 * i]) | (uint32_t)E::from_f32(v[2 * i + 1]) << 16;
+            else r.w[i] = __builtin_bit_cast(uint32_t, v[i]);
+        }
+        return r;
+    }
+    __device__ __forceinline__ Piece<E, 8> piece() const { return __builtin_bit_cast(Piece<E, 8>, *this); }
+};
+
+// n elements on from a kernel's argument p, n the same for all lanes.  (A pointer that is put together from scalar registers itself, as by
+// uniform_ptr, is of no address space to the compiler: flat accesses, which count as LDS ones too, at 64-bit addresses in vector registers.)
+template <typename T>
+static __device__ __forceinline__ T *uniform_on(T *p, int64_t n) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)n), hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)n >> 32));
+    return p + (int64_t)((uint64_t)hi << 32 | lo);
+}
+// p is the same for all lanes, the offset 32 bits of each lane's own: one register an address
+template <typename T>
+static __device__ __forceinline__ T *bytes_on(T *p, uint32_t offset) {
+    using Byte = std::conditional_t<std::is_const<T>::value, const uint8_t, uint8_t>;
+    return reinterpret_cast<T *>(reinterpret_cast<Byte *>(p) + offset);
+}
+
 // What follows the sums of a wave's 64 channels x 16 FM tokens, from channel n0 of token m0 on: the lane's token of fragment j is
 // m0 + 16 j + lane % 16, its channels 8 (lane / 16) .. + 7 and the same 32 further on (channel_of_row).
 template <typename P, int ACT, int FM>
 static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typename P::Acc (&acc)[4][FM], int m0, int n0) {
     using E = typename P::Out;
     using Raw = typename E::Raw;
-    using Eight = Piece<E, 8>;
+    using Row8 = Eight<E>;
     constexpr int B = FM < 4 ? FM : 4;
     const Raw *bias_row = static_cast<const Raw *>(a.bias), *gate_rows = static_cast<const Raw *>(a.gate);
     const int lane = threadIdx.x & 63, row = lane & 15, col = 8 * (lane >> 4);
     if (m0 >= a.M || n0 >= a.N) return;
     const bool shared_gate = a.gate && m0 / a.gate_rows == (min(m0 + 16 * FM, a.M) - 1) / a.gate_rows;   // one row for all tokens
-    const uint32_t off_y = row * (uint32_t)a.ldy + col, off_r = row * (uint32_t)a.ldr + col;             // elements
-    Raw *y = const_cast<Raw *>(uniform_ptr(static_cast<Raw *>(a.y) + (m0 * a.ldy + n0)));
-    const Raw *res = a.residual ? uniform_ptr(static_cast<const Raw *>(a.residual) + (m0 * a.ldr + n0)) : nullptr;
+    const uint32_t off_y = (row * (uint32_t)a.ldy + col) * (uint32_t)sizeof(Raw), off_r = (row * (uint32_t)a.ldr + col) * (uint32_t)sizeof(Raw);   // bytes
+    Raw *y = uniform_on(static_cast<Raw *>(a.y), m0 * a.ldy + n0);
+    const Raw *res = a.residual ? uniform_on(static_cast<const Raw *>(a.residual), m0 * a.ldr + n0) : nullptr;
     // scales of 8 channels (from n on, `count` of them) and of the tokens
     struct Scales {
         float e[P::kScaled ? 8 : 1];
@@ -105,80 +152,98 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
         }
         return s;
     };
-    auto values = [&](float (&v)[8], int h, int j, const Eight &bias, const Scales &s) {
+    auto values = [&](float (&v)[8], int h, int j, const Row8 &bias, const Scales &s) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const auto sum = acc[2 * h + i / 4][j][i & 3];
-            if constexpr (P::kScaled) v[i] = activate<ACT>(fmaf((float)sum * s.e[i], token_scale[j], E::to_f32(bias.e[i])));
-            else v[i] = activate<ACT>(sum + E::to_f32(bias.e[i]));
+            if constexpr (P::kScaled) v[i] = activate<ACT>(fmaf((float)sum * s.e[i], token_scale[j], bias.at(i)));
+            else v[i] = activate<ACT>(sum + bias.at(i));
         }
     };
-    auto times = [](float (&v)[8], const Eight &p) {
+    auto times = [](float (&v)[8], const Row8 &p) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= E::to_f32(p.e[i]);
+        for (int i = 0; i < 8; ++i) v[i] *= p.at(i);
     };
-    auto plus = [](float (&v)[8], const Eight &p) {
+    auto plus = [](float (&v)[8], const Row8 &p) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += E::to_f32(p.e[i]);
+        for (int i = 0; i < 8; ++i) v[i] += p.at(i);
     };
-    auto rounded = [](const float (&v)[8]) {
-        Eight o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o.e[i] = E::from_f32(v[i]);
-        return o;
-    };
-    if (m0 + 16 * FM <= a.M && n0 + 64 <= a.N) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int n = n0 + 32 * h + col;
-            const Scales s = scales(n, 8);
-            Eight bias = {}, gate;
-            if (a.bias) bias = load_piece<E, 8>(bias_row + n, 8);
-            if (shared_gate) gate = load_piece<E, 8>(gate_rows + (m0 / a.gate_rows) * a.ldg + n, 8);
-            // the residual of B tokens is on its way while the B before are worked off (y may be the residual: the compiler could not
-            // move a load above a store)
-            Eight r[2][B];
-            auto fetch = [&](int j0) {
-#pragma unroll
-                for (int j = 0; j < B; ++j) r[(j0 / B) & 1][j] = load_piece<E, 8>(res + 16 * (j0 + j) * a.ldr + 32 * h + off_r, 8);
+    if (m0 + 16 * FM <= a.M && n0 + 64 <= a.N && (!a.gate || shared_gate)) {
+        // Loads come back behind the stores in front of them, and behind a branch around a load the compiler waits for all of both.  So each
+        // combination of gate and residual has its own way without branches, and what the next chunk of B tokens is made of is requested before the
+        // stores of the present one, the residual (which y may be: the compiler could not move its loads above a store) two chunks ahead.
+        const auto whole = [&](auto gated, auto added) {
+            constexpr bool GATE = decltype(gated)::value, RES = decltype(added)::value;
+            constexpr int C = FM / B;                        // chunks of 32 channels
+            Scales s;
+            Row8 bias, gate, r[2][B], out[B];
+            auto vectors = [&](int h) {
+                const int n = n0 + 32 * h + col;
+                s = scales(n, 8);
+                bias = Row8();
+                if (a.bias) bias = Row8::load(bias_row + n, 8);
+                if constexpr (GATE) gate = Row8::load(gate_rows + (m0 / a.gate_rows) * a.ldg + n, 8);
             };
-            if (res) fetch(0);
+            auto fetch = [&](int c) {
 #pragma unroll
-            for (int j0 = 0; j0 < FM; j0 += B) {
-                if (j0 + B < FM && res) fetch(j0 + B);
+                for (int j = 0; j < B; ++j) r[c & 1][j] = Row8::load(bytes_on(res + 16 * (c % C * B + j) * a.ldr + 32 * (c / C), off_r), 8);
+            };
+            vectors(0);
+            if constexpr (RES) {
+                fetch(0);
+                fetch(1);
+            }
+#pragma unroll
+            for (int c = 0; c < 2 * C; ++c) {
+                const int h = c / C, j0 = c % C * B;
 #pragma unroll
                 for (int j = 0; j < B; ++j) {
                     float v[8];
                     values(v, h, j0 + j, bias, s);
-                    if (a.gate) {
-                        if (!shared_gate) gate = load_piece<E, 8>(gate_rows + ((m0 + 16 * (j0 + j) + row) / a.gate_rows) * a.ldg + n, 8);
-                        times(v, gate);
-                    }
-                    if (res) plus(v, r[(j0 / B) & 1][j]);
-                    Raw *to = y + 16 * (j0 + j) * a.ldy + 32 * h + off_y;
-                    if (a.streaming) store_piece<E, 8, true>(to, rounded(v), 8);
-                    else store_piece<E, 8>(to, rounded(v), 8);
+                    if constexpr (GATE) times(v, gate);
+                    if constexpr (RES) plus(v, r[c & 1][j]);
+                    out[j] = Row8::rounded(v);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                if (c == C - 1) vectors(1);
+                if constexpr (RES)
+                    if (c + 2 < 2 * C) fetch(c + 2);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < B; ++j) {
+                    Raw *to = bytes_on(y + 16 * (j0 + j) * a.ldy + 32 * h, off_y);
+                    if (a.streaming) store_piece<E, 8, true>(to, out[j].piece(), 8);
+                    else store_piece<E, 8>(to, out[j].piece(), 8);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        using std::true_type;
+        using std::false_type;
+        if (a.gate) {
+            if (res) whole(true_type(), true_type());
+            else whole(true_type(), false_type());
+        } else {
+            if (res) whole(false_type(), true_type());
+            else whole(false_type(), false_type());
         }
     } else {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int n = n0 + 32 * h + col, count = min(8, a.N - n);
-            Eight bias = {};
+            Row8 bias = {};
             Scales s = {};
             if (count > 0) s = scales(n, count);
-            if (a.bias && count > 0) bias = load_piece<E, 8>(bias_row + n, count);
+            if (a.bias && count > 0) bias = Row8::load(bias_row + n, count);
 #pragma unroll
             for (int j = 0; j < FM; ++j) {
                 const int m = m0 + 16 * j + row;
                 if (m < a.M && count > 0) {
                     float v[8];
                     values(v, h, j, bias, s);
-                    if (a.gate) times(v, load_piece<E, 8>(gate_rows + (m / a.gate_rows) * a.ldg + n, count));
-                    if (res) plus(v, load_piece<E, 8>(res + 16 * j * a.ldr + 32 * h + off_r, count));
-                    store_piece<E, 8>(y + 16 * j * a.ldy + 32 * h + off_y, rounded(v), count);
+                    if (a.gate) times(v, Row8::load(gate_rows + (m / a.gate_rows) * a.ldg + n, count));
+                    if (res) plus(v, Row8::load(bytes_on(res + 16 * j * a.ldr + 32 * h, off_r), count));
+                    store_piece<E, 8>(bytes_on(y + 16 * j * a.ldy + 32 * h, off_y), Row8::rounded(v).piece(), count);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -387,8 +452,9 @@ static __device__ __forceinline__ void lds_direct_load16_at(const void *p, uint3
 __device__ uint4 zero_piece;   // what the pieces past K of the last slice are read from
 
 // Tiles of 64 WN channels x 16 FM WM tokens, WN x WM waves of 64 channels x 16 FM tokens each; slices of 128 bytes of K.
-// Weights have three slices in LDS, tokens two: while a slice is multiplied, the next is there, the weights of the one after it
-// come in, and its tokens follow as soon as those of the present slice have been read.  (What bounds the loop on a full chip is the way from
+// Tokens have three slices in LDS, weights two: while a slice is multiplied, the next is there, the tokens of the one after it
+// come in, and its weights follow as soon as those of the present slice have been read.  (The tokens are what comes from further away; with
+// three slices of weights in place of tokens 8-bit 32760 x 13824 x 5120 took 1734 to 1810 us in place of 1693 to 1757, 32760 x 8960 x 1536 360 in place of 351.)  (What bounds the loop on a full chip is the way from
 // the L2s into LDS, 54 to 69 GB/s per compute unit where 32 of them share panels; it must not run dry.)
 // A slice is worked off in phases of 16 matrix instructions (or fewer), and a phase begins by requesting the fragments of the next one.
 // Before the last phase of a slice, whose fragments are then in registers, stands the slice's one barrier: behind it the next slice is
@@ -401,7 +467,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
     constexpr int LW = BN / 8 / W, LX = BM / 8 / W;          // loads of a wave per slice, 8 rows each
     constexpr int kStores = ACT == kPart || sizeof(typename P::Out::Raw) == 4 ? 4 * FM : 2 * FM;   // of a wave per whole tile, at least
     constexpr uint32_t kUnitW = BN * 128, kUnitX = BM * 128;
-    extern __shared__ uint4 lds[];                           // weights: 3 units, tokens: 2
+    extern __shared__ uint4 lds[];                           // weights: 2 units, tokens: 3
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n_tiles = (a.N + BN - 1) / BN, m_tiles = (a.M + BM - 1) / BM, tiles = n_tiles * m_tiles, items = tiles * a.splits, grid = gridDim.x;
     const int wn = wave % WN * 64, wm = wave / WN * 16 * FM;
@@ -413,7 +479,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
     const int xcds = min(8, grid), xcd = blockIdx.x % xcds, step = (grid - xcd + xcds - 1) / xcds;
     const int share = items / xcds, more = items % xcds;     // (the first XCDs have one more, of workgroups as well as of tiles)
     const int end = share * (xcd + 1) + min(xcd + 1, more);
-    const uint32_t lds_w = lds_address(lds) + wave * (1024 * LW), lds_x = lds_address(lds) + 3 * kUnitW + wave * (1024 * LX);
+    const uint32_t lds_w = lds_address(lds) + wave * (1024 * LW), lds_x = lds_address(lds) + 2 * kUnitW + wave * (1024 * LX);
     const uint8_t *src_w, *src_x;
     uint32_t off_w[LW], off_x[LX];
     const bool spread_w = a.N * a.ldw < (int64_t)1 << 32, spread_x = a.M * a.ldx < (int64_t)1 << 32;   // offsets of 32 bits
@@ -473,7 +539,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
     // fragment reads: LDS row r of 128 bytes holds its 16-byte piece c at c ^ ((r >> 1) & 7), so that the 16 rows that a read takes at
     // once lie in different banks
     const int at = (lane & 15) * 8 + ((lane >> 4) ^ ((lane & 15) >> 1));   // of k-step 0; k-step 1 is piece ^ 4
-    const int at_w = wn * 8 + at, at_x = 3 * (kUnitW / 16) + wm * 8 + at;
+    const int at_w = wn * 8 + at, at_x = 2 * (kUnitW / 16) + wm * 8 + at;
     typename P::Acc acc[4][FM] = {};
     uint4 fw[2][4], fx[2][FH];
     auto read = [&](int sw, int sx, int p) {                 // the fragments of phase p of the slice in these places
@@ -501,7 +567,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
         // STEADY: slices of this tile follow, all within K
         auto slice = [&](int q, auto steady) {
             constexpr bool STEADY = decltype(steady)::value;
-            const int nw = sw == 2 ? 0 : sw + 1, aw = nw == 2 ? 0 : nw + 1;
+            const int nx = sx == 2 ? 0 : sx + 1, ax = nx == 2 ? 0 : nx + 1;
             bool loads = true;                               // what is loaded two slices ahead
             int lq = q + 2;
             if (!STEADY && lq >= slices) {
@@ -513,14 +579,14 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
             for (int p = 0; p < PH; ++p) {
                 if (p < PH - 1) {
                     read(sw, sx, p + 1);
-                    if (p == 0 && loads) load_w(lq, aw, STEADY);
+                    if (p == 0 && loads) load_x(lq, ax, STEADY);
                 } else if (STEADY || q + 1 < slices || next < end) {
                     if (!STEADY && !loads) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                    else if (STEADY || !(stored && q == 0)) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LW) : "memory");
-                    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LW + kStores) : "memory");
+                    else if (STEADY || !(stored && q == 0)) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LX) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LX + kStores) : "memory");
                     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                    if (loads) load_x(lq, sx, STEADY);
-                    if (STEADY || q + 1 < slices) read(nw, sx ^ 1, 0);   // (of the next tile: behind the outputs)
+                    if (loads) load_w(lq, sw, STEADY);
+                    if (STEADY || q + 1 < slices) read(sw ^ 1, nx, 0);   // (of the next tile: behind the outputs)
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -529,8 +595,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
                     for (int j = 0; j < FH; ++j) acc[i][(p % NH) * FH + j] = P::mfma(fw[p / NH][i], fx[p & 1][j], acc[i][(p % NH) * FH + j]);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            sw = nw;
-            sx ^= 1;
+            sx = nx;
+            sw ^= 1;
         };
         const int steady = stored ? 1 : 0;
 #pragma unroll 1
@@ -555,7 +621,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
 template <typename P, int ACT, int FM, int WN, int WM>
 int launch_tiles(const LinearArgs &a, int per_cu, int group_n, hipStream_t stream) {
     constexpr int BN = 64 * WN, BM = 16 * FM * WM;
-    constexpr size_t kLds = (3 * BN + 2 * BM) * 128;
+    constexpr size_t kLds = (2 * BN + 3 * BM) * 128;
     static std::atomic<uint64_t> done{0};
     const auto kernel = linear_tiles<P, ACT, FM, WN, WM>;
     allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kLds, done);
