@@ -12,10 +12,10 @@
 
 namespace dvdq {
 
-size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K) { return workspace_for(M, N, 2 * K); }
+size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K) { return workspace_for(M, N, 2 * K, false); }
 
 int linear_choice(int64_t M, int64_t N, int64_t K, bool any) {
-    if (few_tokens(M, N, 2 * K)) return -1;
+    if (few_tokens(M, N, 2 * K, false)) return -1;
     const LinearPlan p = linear_plan(M, N, 2 * K, any);
     return p.shape + 16 * p.splits + (p.pad_bytes ? 4096 : any ? 8192 : 0);
 }

@@ -31,26 +31,26 @@ struct Op16 {                          // 16-bit elements, sums in fp32
         else
             return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
     }
-    // 16 bytes at any element's address, of which `left` belong to the row
-    static __device__ __forceinline__ uint4 load(const uint8_t *p, int left) {
-        return __builtin_bit_cast(uint4, load_piece<E>(reinterpret_cast<const typename E::Raw *>(p), left / 2));
-    }
+    static constexpr int kBytes = 2;
 };
 template <typename E>
 struct Op8 {                           // 8-bit codes, exact sums, a scale per token and per channel
     using Out = E;
     using Acc = v4i;
     static constexpr bool kScaled = true;
-    struct Code {
-        using Raw = int8_t;
-    };
-    static __device__ __forceinline__ v4i mfma(uint4 a, uint4 b, v4i c) {
+    static constexpr int kBytes = 1;    static __device__ __forceinline__ v4i mfma(uint4 a, uint4 b, v4i c) {
         return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, a), __builtin_bit_cast(v4i, b), c, 0, 0, 0);
     }
-    static __device__ __forceinline__ uint4 load(const uint8_t *p, int left) {
-        return __builtin_bit_cast(uint4, load_piece<Code, 16>(reinterpret_cast<const int8_t *>(p), left));
-    }
 };
+// 16 bytes at any element's address, of which `left` belong to the row, whose length is K
+template <typename P>
+static __device__ __forceinline__ uint4 load_operand(const uint8_t *p, int left, int K) {
+    struct __attribute__((packed, aligned(P::kBytes))) Sixteen {
+        uint32_t w[4];
+    };
+    if (left >= 16) return __builtin_bit_cast(uint4, *reinterpret_cast<const Sixteen *>(p));
+    return load_end<P::kBytes>(p, left, K >= 16);
+}
 
 struct LinearArgs {
     const uint8_t *x, *w;
@@ -79,15 +79,18 @@ struct Eight {
         if constexpr (kWords == 2) return E::to_f32((uint16_t)(w[i / 2] >> 16 * (i % 2)));
         else return __builtin_bit_cast(float, w[i]);
     }
+    // n of them, at least one; what comes past those is not to be used
     static __device__ __forceinline__ Eight load(const typename E::Raw *p, int n) {
         if (n >= 8) return __builtin_bit_cast(Eight, *reinterpret_cast<const Piece<E, 8> *>(p));
-        Eight r = {};
+        uint32_t e[8];                                       // (the last one in the place of those past it: no load hangs on a condition)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) {
-                if constexpr (kWords == 2) r.w[i / 2] |= (uint32_t)p[i] << 16 * (i % 2);
-                else r.w[i] = __builtin_bit_cast(uint32_t, p[i]);
-            }
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (kWords == 2) e[i] = p[min(i, n - 1)];
+            else e[i] = __builtin_bit_cast(uint32_t, p[min(i, n - 1)]);
+        }
+        Eight r;
+#pragma unroll
+        for (int i = 0; i < 2 * kWords; ++i) r.w[i] = kWords == 2 ? e[2 * i % 8] | e[(2 * i + 1) % 8] << 16 : e[i];
         return r;
     }
     static __device__ __forceinline__ Eight rounded(const float (&v)[8]) {
@@ -145,9 +148,8 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
         if constexpr (P::kScaled) {
 #pragma unroll
             for (int i = 0; i < 8; i += 4) {
-                const Piece<Fp32> p = load_piece<Fp32>(a.w_scale + n + i, count - i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s.e[i + e] = p.e[e];
+                #pragma unroll
+                for (int e = 0; e < 4; ++e) s.e[i + e] = a.w_scale[count == 8 ? n + i + e : min(n + i + e, a.N - 1)];
             }
         }
         return s;
@@ -231,21 +233,31 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int n = n0 + 32 * h + col, count = min(8, a.N - n);
+            if (count <= 0) continue;
+            const Scales s = scales(n, count);
             Row8 bias = {};
-            Scales s = {};
-            if (count > 0) s = scales(n, count);
-            if (a.bias && count > 0) bias = Row8::load(bias_row + n, count);
+            if (a.bias) bias = Row8::load(bias_row + n, count);
 #pragma unroll
-            for (int j = 0; j < FM; ++j) {
-                const int m = m0 + 16 * j + row;
-                if (m < a.M && count > 0) {
-                    float v[8];
-                    values(v, h, j, bias, s);
-                    if (a.gate) times(v, Row8::load(gate_rows + (m / a.gate_rows) * a.ldg + n, count));
-                    if (res) plus(v, Row8::load(bytes_on(res + 16 * j * a.ldr + 32 * h, off_r), count));
-                    store_piece<E, 8>(bytes_on(y + 16 * j * a.ldy + 32 * h, off_y), Row8::rounded(v).piece(), count);
+            for (int j0 = 0; j0 < FM; j0 += B) {
+                Row8 r[B] = {};
+                if (res)
+#pragma unroll
+                    for (int j = 0; j < B; ++j) {
+                        const uint32_t up = max(m0 + 16 * (j0 + j) + row - (a.M - 1), 0);   // (tokens past the last read the last one's)
+                        r[j] = Row8::load(bytes_on(res + 16 * (j0 + j) * a.ldr + 32 * h, off_r) - up * a.ldr, count);
+                    }
+#pragma unroll
+                for (int j = 0; j < B; ++j) {
+                    const int m = m0 + 16 * (j0 + j) + row;
+                    if (m < a.M) {
+                        float v[8];
+                        values(v, h, j0 + j, bias, s);
+                        if (a.gate) times(v, Row8::load(gate_rows + (m / a.gate_rows) * a.ldg + n, count));
+                        if (res) plus(v, r[j]);
+                        store_piece<E, 8>(bytes_on(y + 16 * (j0 + j) * a.ldy + 32 * h, off_y), Row8::rounded(v).piece(), count);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
-                __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
@@ -287,8 +299,8 @@ __global__ __launch_bounds__(256, 2) void linear_any(LinearArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = row0 + 32 * i;
-            pw[i] = P::load(a.w + min(n0 + channel_of_row(row), a.N - 1) * a.ldw + k, count);
-            px[i] = P::load(a.x + min(m0 + row, a.M - 1) * a.ldx + k, count);
+            pw[i] = load_operand<P>(a.w + min(n0 + channel_of_row(row), a.N - 1) * a.ldw + k, count, a.K);
+            px[i] = load_operand<P>(a.x + min(m0 + row, a.M - 1) * a.ldx + k, count, a.K);
         }
     };
     if (q0 < q1) load(q0);
@@ -329,7 +341,12 @@ __global__ __launch_bounds__(256, 2) void linear_any(LinearArgs a) {
 // 1 x 1536 x 4608 6.5 and 11.9, 16 x 1536 x 13824 15.0 and 18.2, 2 x 5120 x 30720 57 and 67.  Few channels leave compute units idle and long rows their
 // waves with too little in flight: 8 x 13824 x 128 22 and 15, 16 x 5120 x 5120 23 and 19, 2 x 13824 x 5120 36 and 36; these are tiles.
 constexpr int kFewWaves = 8;
-inline bool few_tokens(int64_t M, int64_t N, int64_t K) { return M <= 16 && (K <= 8192 || N >= 16384); }   // K: bytes of a row
+// 8-bit codes, us, this and tiles: 1 x 13824 x 5120 19.0 and 24.8, 8 x 13824 x 5120 23.9 and 24.9, 16 x 13824 x 5120 28.8 and 24.3 (a step loads as many bytes of
+// tokens as of weights by then), 16 x 5120 x 5120 11.5 and 13.3, 16 x 5120 x 30720 47 and 41, 8 x 5120 x 30720 37 and 41, 16 x 8960 x 1536 10.2 and 12.3,
+// 8 x 13824 x 512 12.5 and 12.2, 16 x 13824 x 512 14.2 and 12.0.  32 tokens as two groups: 5120 x 5120 16 and 14.
+inline bool few_tokens(int64_t M, int64_t N, int64_t K, bool codes) {   // K: bytes of a row
+    return codes ? M <= 8 || (M <= 16 && K <= 12288 && N * K <= (int64_t)1 << 26) : M <= 16 && (K <= 8192 || N >= 16384);
+}
 template <typename P, int ACT>
 __global__ __launch_bounds__(512) void linear_few(LinearArgs a) {
     using E = typename P::Out;
@@ -351,8 +368,8 @@ __global__ __launch_bounds__(512) void linear_few(LinearArgs a) {
         for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                pw[i][h] = P::load(w + (q + i) * 128 + 16 * h, 16);
-                px[i][h] = P::load(x + (q + i) * 128 + 16 * h, 16);
+                pw[i][h] = load_operand<P>(w + (q + i) * 128 + 16 * h, 16, a.K);
+                px[i][h] = load_operand<P>(x + (q + i) * 128 + 16 * h, 16, a.K);
             }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
@@ -365,8 +382,8 @@ __global__ __launch_bounds__(512) void linear_few(LinearArgs a) {
         for (int i = 0; i < AHEAD - 1; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                pw[i][h] = P::load(w + min(q + i, whole - 1) * 128 + 16 * h, 16);
-                px[i][h] = P::load(x + min(q + i, whole - 1) * 128 + 16 * h, 16);
+                pw[i][h] = load_operand<P>(w + min(q + i, whole - 1) * 128 + 16 * h, 16, a.K);
+                px[i][h] = load_operand<P>(x + min(q + i, whole - 1) * 128 + 16 * h, 16, a.K);
             }
 #pragma unroll
         for (int i = 0; i < AHEAD - 1; ++i)
@@ -381,8 +398,8 @@ __global__ __launch_bounds__(512) void linear_few(LinearArgs a) {
             const int k = whole * 128 + 16 * h, left = a.K - k - (lane >> 4) * 32;
             uint4 pw = {}, px = {};
             if (left > 0) {
-                pw = P::load(w + k, left);
-                px = P::load(x + k, left);
+                pw = load_operand<P>(w + k, left, a.K);
+                px = load_operand<P>(x + k, left, a.K);
             }
             acc[h] = P::mfma(pw, px, acc[h]);
         }
@@ -403,19 +420,30 @@ __global__ __launch_bounds__(512) void linear_few(LinearArgs a) {
     static_cast<Raw *>(a.y)[m * a.ldy + n] = E::from_f32(v);
 }
 
-// Rows of K bytes at any address -> rows of `pitch` bytes, a multiple of 128, zero past K: activations (rows_x of them), then weights.
+// Rows of K bytes at any address -> rows of `pitch` bytes, a multiple of 128, zero past K: activations (rows_x of them), then weights.  A
+// workgroup has `rows` rows, whose pieces are numbered through: piece i is in row i * mul >> 32, mul = 2^32 / pieces rounded up, which is exact for
+// 16 rows of fewer than 2^14 pieces; longer rows have a workgroup each (mul = 0).
 template <typename P>
 __global__ __launch_bounds__(256) void linear_pad(const uint8_t *x, int64_t ldx, int rows_x, const uint8_t *w, int64_t ldw, int rows_w, int K,
-                                                  int pitch, uint8_t *out) {
+                                                  int pitch, int rows, uint32_t mul, uint8_t *out) {
     const uint32_t pieces = (uint32_t)pitch / 16;
-    const int64_t total = (int64_t)(rows_x + rows_w) * pieces;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += gridDim.x * (int64_t)256) {
-        const int64_t row = i / pieces;
-        const int k = (int)(i - row * pieces) * 16;
-        const uint8_t *src = row < rows_x ? x + row * ldx : w + (row - rows_x) * ldw;
-        uint4 p = {};
-        if (k < K) p = P::load(src + k, min(16, K - k));
-        reinterpret_cast<uint4 *>(out)[i] = p;
+    const int64_t row0 = (int64_t)blockIdx.x * rows;
+    const uint32_t here = pieces * (uint32_t)min((int64_t)rows, rows_x + (int64_t)rows_w - row0);
+    uint4 *to = reinterpret_cast<uint4 *>(out) + row0 * pieces;
+    constexpr int AHEAD = 4;
+    for (uint32_t i = threadIdx.x; i < here; i += 256 * AHEAD) {
+        uint4 p[AHEAD];
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            const uint32_t at = i + 256 * e, r = __umulhi(at, mul);
+            const int k = (int)(at - r * pieces) * 16;
+            const int64_t row = row0 + r;
+            p[e] = uint4();
+            if (at < here && k < K) p[e] = load_operand<P>((row < rows_x ? x + row * ldx : w + (row - rows_x) * ldw) + k, min(16, K - k), K);
+        }
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e)
+            if (i + 256 * e < here) to[i + 256 * e] = p[e];
     }
 }
 
@@ -712,8 +740,8 @@ int launch_product(const LinearArgs &a, const LinearPlan &p, bool any, hipStream
 // addresses and pitches of an operand that tiles read straight into LDS
 inline bool whole_pieces(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 15) == 0 && ld < (int64_t)1 << 23; }
 
-inline size_t workspace_for(int64_t M, int64_t N, int64_t K) {
-    if (few_tokens(M, N, K)) return 0;
+inline size_t workspace_for(int64_t M, int64_t N, int64_t K, bool codes) {
+    if (few_tokens(M, N, K, codes)) return 0;
     const size_t any = plan_bytes(linear_plan(M, N, K, true));   // (addresses and pitches are not known here)
     return K % 16 == 0 ? std::max(any, plan_bytes(linear_plan(M, N, K, false))) : any;
 }
@@ -721,7 +749,7 @@ inline size_t workspace_for(int64_t M, int64_t N, int64_t K) {
 // The product of operands P; those of the output's type come into play in the last of the launches only.
 template <typename P, typename Parts, int ACT>
 int launch_few_or_tiles(LinearArgs a, void *workspace, hipStream_t stream) {
-    if (few_tokens(a.M, a.N, a.K)) {
+    if (few_tokens(a.M, a.N, a.K, P::kScaled)) {
         linear_few<P, ACT><<<dim3((unsigned)((a.N + 15) / 16)), 64 * kFewWaves, kFewWaves * 1024, stream>>>(a);
         return check_launch();
     }
@@ -731,8 +759,10 @@ int launch_few_or_tiles(LinearArgs a, void *workspace, hipStream_t stream) {
     if (p.pad_bytes) {
         const int pitch = (a.K + 127) / 128 * 128;
         uint8_t *rows = static_cast<uint8_t *>(workspace);
-        const int64_t blocks = std::min((int64_t)256 * 32, ((int64_t)(a.M + a.N) * (pitch / 16) + 255) / 256);
-        linear_pad<Parts><<<dim3((unsigned)blocks), 256, 0, stream>>>(a.x, a.ldx, a.M, a.w, a.ldw, a.N, a.K, pitch, rows);
+        const int pieces = pitch / 16, at_once = pieces < 1 << 14 ? 16 : 1;
+        const uint32_t mul = at_once == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + pieces - 1) / pieces);
+        const int64_t groups = ((int64_t)a.M + a.N + at_once - 1) / at_once;
+        linear_pad<Parts><<<dim3((unsigned)groups), 256, 0, stream>>>(a.x, a.ldx, a.M, a.w, a.ldw, a.N, a.K, pitch, at_once, mul, rows);
         const int rc = check_launch();
         if (rc != DVDQ_OK) return rc;
         a.x = rows, a.w = rows + (int64_t)a.M * pitch;

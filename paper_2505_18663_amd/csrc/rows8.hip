@@ -148,20 +148,12 @@ static __device__ __forceinline__ Scale scale_from(uint32_t top_bits) {
     return {(double)top, 0.0f, top_bits < 0x7F800000u, top < kTiny};
 }
 
-// 16 bytes of a row as four words, which stay four registers also where the piece across a row's end is put together by element (as an array of
-// elements that was 8: 92 registers for three pieces of the norm in place of 70).
+// 16 bytes of a row as four words, which stay four registers also where branches meet (as an array of elements each has a register).
 template <typename E>
-static __device__ __forceinline__ uint4 load_words(const typename E::Raw *p, int n) {
-    constexpr int V = E::kVec;
-    if (n >= V) return __builtin_bit_cast(uint4, *reinterpret_cast<const Piece<E> *>(p));
-    uint32_t w[4] = {};
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-        if (e < n) {
-            if constexpr (V == 8) w[e / 2] |= (uint32_t)p[e] << 16 * (e % 2);
-            else w[e] = __builtin_bit_cast(uint32_t, p[e]);
-        }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+static __device__ __forceinline__ uint4 load_words(const typename E::Raw *p, int n, bool whole_before) {
+    constexpr int kBytes = sizeof(typename E::Raw);
+    if (n >= E::kVec) return __builtin_bit_cast(uint4, *reinterpret_cast<const Piece<E> *>(p));
+    return load_end<kBytes>(reinterpret_cast<const uint8_t *>(p), n * kBytes, whole_before);
 }
 static __device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 template <typename E>
@@ -221,13 +213,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
     uint32_t row = (uint32_t)(there ? mine : a.rows - 1);
     if (T >= 64) row = __builtin_amdgcn_readfirstlane(row);
     const Row<E, MODE> r(a, row);
+    const bool long_row = a.C >= V;
     uint4 px[NP], ps[NP], pw[NP];
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int c = (l + T * i) * V, n = i < kWhole ? V : a.C - c;
-        px[i] = load_words<E>(r.x + c, n);
-        if (r.second) ps[i] = load_words<E>(r.second + c, n);
-        if (is_norm(MODE) && r.weight) pw[i] = load_words<E>(r.weight + c, n);
+        px[i] = load_words<E>(r.x + c, n, long_row);
+        if (r.second) ps[i] = load_words<E>(r.second + c, n, long_row);
+        if (is_norm(MODE) && r.weight) pw[i] = load_words<E>(r.weight + c, n, long_row);
     }
     float z[NP][V], sum = 0.0f, top = 0.0f, up_top = 0.0f;
     if constexpr (MODE == kQuantAct) {
