@@ -422,7 +422,7 @@ __global__ __launch_bounds__(512) void linear_few(LinearArgs a) {
 
 // Rows of K bytes at any address -> rows of `pitch` bytes, a multiple of 128, zero past K: activations (rows_x of them), then weights.  A
 // workgroup has `rows` rows, whose pieces are numbered through: piece i is in row i * mul >> 32, mul = 2^32 / pieces rounded up, which is exact for
-// 16 rows of fewer than 2^14 pieces; longer rows have a workgroup each (mul = 0).
+// the 512 pieces that rows share a workgroup up to; longer rows have one each (mul = 0).
 template <typename P>
 __global__ __launch_bounds__(256) void linear_pad(const uint8_t *x, int64_t ldx, int rows_x, const uint8_t *w, int64_t ldw, int rows_w, int K,
                                                   int pitch, int rows, uint32_t mul, uint8_t *out) {
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(256) void linear_pad(const uint8_t *x, int64_t ldx,
     const int64_t row0 = (int64_t)blockIdx.x * rows;
     const uint32_t here = pieces * (uint32_t)min((int64_t)rows, rows_x + (int64_t)rows_w - row0);
     uint4 *to = reinterpret_cast<uint4 *>(out) + row0 * pieces;
-    constexpr int AHEAD = 4;
+    constexpr int AHEAD = 2;
     for (uint32_t i = threadIdx.x; i < here; i += 256 * AHEAD) {
         uint4 p[AHEAD];
 #pragma unroll
@@ -759,7 +759,7 @@ int launch_few_or_tiles(LinearArgs a, void *workspace, hipStream_t stream) {
     if (p.pad_bytes) {
         const int pitch = (a.K + 127) / 128 * 128;
         uint8_t *rows = static_cast<uint8_t *>(workspace);
-        const int pieces = pitch / 16, at_once = pieces < 1 << 14 ? 16 : 1;
+        const int pieces = pitch / 16, at_once = std::max(1, std::min(16, 512 / pieces));
         const uint32_t mul = at_once == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + pieces - 1) / pieces);
         const int64_t groups = ((int64_t)a.M + a.N + at_once - 1) / at_once;
         linear_pad<Parts><<<dim3((unsigned)groups), 256, 0, stream>>>(a.x, a.ldx, a.M, a.w, a.ldw, a.N, a.K, pitch, at_once, mul, rows);
