@@ -60,6 +60,23 @@ def test_sizes(size, dtype):
     check(args, f"{size} all", on, dtype=dtype, bias=tensor(g, N, dtype=dtype), act=dvdq.ACT_GELU_TANH, gate=gate, residual=tensor(g, M, N, dtype=dtype))
 
 
+# a size for each shape of tile (0: 256 x 256 .. 4: 64 x 64), whole and in parts of K: which one a size takes is that of the 16-bit product with as many bytes
+# in a row (see test_rows8_linear8.py)
+WAYS = {(0, 1): (2600, 5120, 784), (0, 3): (2600, 1540, 13824), (1, 1): (12000, 260, 1168), (1, 4): (6200, 136, 8208), (2, 1): (12000, 136, 48),
+        (2, 11): (70, 1540, 8208), (3, 1): (70, 9000, 48), (3, 7): (70, 1540, 4112), (4, 1): (40, 48, 48), (4, 4): (40, 48, 2064)}
+
+
+@pytest.mark.parametrize("way", WAYS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_every_shape_of_tile(way, dtype):
+    M, N, K = WAYS[way]
+    g = gen(M)
+    args = operands(g, M, N, K)
+    bias, gate, residual = tensor(g, N, dtype=dtype), tensor(g, 2, N, dtype=dtype), tensor(g, M, N, dtype=dtype)
+    for kw in ({}, {"gate": gate}, {"residual": residual}, {"gate": gate, "residual": residual, "act": dvdq.ACT_SILU}, {"gate": residual, "residual": residual}):
+        check(args, f"{way} {dtype} {list(kw)}", DEV, dtype=dtype, bias=bias, **kw)
+
+
 @pytest.mark.parametrize("M", [3, 40, 700])
 @pytest.mark.parametrize("act", [0, 1, 2, 3])
 def test_epilogues(M, act):

@@ -98,6 +98,36 @@ def test_values_a_hair_from_a_border():
     check_codes(codes, scale, x.cpu().double() * up.cpu().double(), 1.0, 0.0, "hair")
 
 
+@pytest.mark.parametrize("C", [30, 250, 1533, 2048, 5120, 9001, 13824, 16384, 40001])
+def test_rows_full_of_values_next_to_borders(C):
+    """Every value within a few units of its last digit of the border between two codes, with and without a second factor, behind a norm's weight and behind
+    each activation: the codes of 64-bit arithmetic all the same."""
+    g = gen(C)
+    rows = 6
+    k = torch.randint(0, 127, (rows, C), generator=g, device=DEV).double() + 0.5
+    sign = torch.randint(0, 2, (rows, C), generator=g, device=DEV) * 2.0 - 1
+    off = 1 + torch.randint(-3, 4, (rows, C), generator=g, device=DEV) * 2.0 ** -23
+    x = (k * sign * off).float()
+    x[:, C // 3] = 127.0
+    check_codes(*dvdq.quant8(x), x.cpu().double(), 1.0, 0.0, f"{C}")
+    second = torch.exp(0.3 * tensor(g, rows, C))
+    y = (x.double() / second.double()).float()                                # the product with `second` is x again, to 24 digits
+    y[:, C // 3] = 127.5 / second[:, C // 3]
+    check_codes(*dvdq.quant8(y, up=second), y.cpu().double() * second.cpu().double(), 1.0, 0.0, f"{C} up")
+    w = second[0].contiguous()
+    z, root, _, err = norm64(x / w, w)
+    check_codes(*dvdq.rms_norm_quant(x / w, w), z, 1 / root, err, f"{C} norm")
+    for act in (dvdq.ACT_SILU, dvdq.ACT_GELU_TANH, dvdq.ACT_GELU):
+        a = tensor(g, rows, C, scale=2.0)
+        a[:, C // 3] = 9.0
+        up = (k * sign / act64(a.double(), act)).float()
+        up[:, C // 3] = 127.0 / 9.0
+        z = act64(a.cpu().double(), act) * up.cpu().double()
+        keep = z.abs() <= z[:, C // 3].abs()[:, None]                         # (a value just above would be the largest)
+        z, up = torch.where(keep, z, 0.0 * z), torch.where(keep.to(DEV), up, 0.0 * up)
+        check_codes(*dvdq.quant8(a, up=up, act=act), z, 1.0, 0.0, f"{C} act {act}", loose=True)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("C", [40, 700, 9000, 40000])
 def test_rows_of_zeros_nans_and_infinities(dtype, C):

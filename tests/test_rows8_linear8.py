@@ -80,3 +80,26 @@ def test_the_binding_refuses_what_is_not_on_a_gpu():
     for f in (lambda: dvdq.rms_norm(x), lambda: dvdq.rms_norm_quant(x), lambda: dvdq.quant8(x), lambda: dvdq.linear8(c, s, c, s)):
         with pytest.raises(TypeError, match="expected a CUDA/HIP tensor"):
             f()
+
+
+def test_the_sizes_that_stand_for_each_shape_of_tile_take_it():
+    from test_gpu_linear8 import WAYS
+    for (shape, parts), (M, N, K) in WAYS.items():
+        assert dvdq.bench_linear_choice(M, N, K // 2) == shape + 16 * parts, (M, N, K)
+        bn, bm = {0: (256, 256), 1: (256, 128), 2: (128, 128), 3: (128, 64), 4: (64, 64)}[shape]
+        need = -(-M // bm) * -(-N // bn) * parts * bm * bn * 4 if parts > 1 else 0
+        assert dvdq.linear8_workspace_bytes(M, N, K) >= need
+    assert {shape for shape, _ in WAYS} == set(range(5))
+    assert dvdq.linear8_workspace_bytes(8, 5120, 13824) == 0 and dvdq.linear8_workspace_bytes(16, 5120, 5120) == 0    # few tokens: straight from the weights
+
+
+def test_the_workspace_holds_whatever_way_the_addresses_ask_for():
+    """Rows that are no whole pieces are copied, or read through registers, in parts of K: the size is for the larger."""
+    for M, N, K in ((40, 48, 1168), (600, 5120, 4001), (33, 65, 1000), (300, 77, 5000)):
+        for any_ in (False, True):
+            c = dvdq.bench_linear_choice(M, N, (K + 1) // 2, any_ or K % 16 != 0)
+            shape, parts, pad = c % 16, c // 16 % 256, bool(c & 4096)
+            bn, bm = {0: (256, 256), 1: (256, 128), 2: (128, 128), 3: (128, 64), 4: (64, 64)}[shape]
+            need = -(-M // bm) * -(-N // bn) * parts * bm * bn * 4 if parts > 1 else 0
+            need += (M + N) * (-(-K // 128) * 128) if pad else 0
+            assert dvdq.linear8_workspace_bytes(M, N, K) >= need, (M, N, K)
