@@ -363,50 +363,88 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
 // Longer rows: a workgroup per row, which it reads again for each step.
 template <typename E, int MODE>
 __global__ __launch_bounds__(1024) void row_long(RowArgs a) {
-    constexpr int T = 1024;
+    constexpr int T = 1024, V = E::kVec;
     __shared__ uint64_t lds[32];
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const Row<E, MODE> r(a, (uint32_t)row);
-        float sum = 0.0f;
-        uint32_t top_bits = 0;
-        for (int c = threadIdx.x; c < a.C; c += T) {
-            const float v = r.value(c, false);
-            if (is_norm(MODE)) sum += v * v;
-            if (MODE != kNorm) top_bits = max(top_bits, __builtin_bit_cast(uint32_t, r.z32(c, v)) & 0x7FFFFFFFu);
+        // the values and z of the n elements from c on, zero past them
+        const auto piece = [&](int c, int n, float (&v)[V], float (&z)[V]) {
+            const uint4 px = load_words<E>(r.x + c, n, true);
+            uint4 ps = {}, pw = {};
+            if (r.second) ps = load_words<E>(r.second + c, n, true);
+            if (is_norm(MODE) && r.weight) pw = load_words<E>(r.weight + c, n, true);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                v[e] = element<E>(px, e);
+                if (is_norm(MODE)) {
+                    if (r.second) v[e] = E::to_f32(E::from_f32(v[e] + element<E>(ps, e)));
+                    z[e] = r.weight ? v[e] * element<E>(pw, e) : v[e];
+                } else {
+                    z[e] = MODE == kQuantAct ? act32(v[e], a.act) : v[e];
+                    if (r.second) z[e] *= element<E>(ps, e);
+                }
+            }
+        };
+        float v[V], z[V], sum = 0.0f, top = 0.0f;
+        for (int c = threadIdx.x * V; c < a.C; c += T * V) {
+            piece(c, a.C - c, v, z);
+            if (is_norm(MODE))
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum = fmaf(v[e], v[e], sum);
+            if (MODE != kNorm)
+#pragma unroll
+                for (int e = 0; e < V; e += 2) top = maximum3(z[e], z[e + 1], top);
         }
         float factor = 1.0f;
         if (is_norm(MODE)) factor = rsqrtf(fmaf(over_row<T>(sum, Add(), lds, turn), a.share, a.eps));
         Scale s = {};
         if (MODE != kNorm) {
-            s = scale_from(over_row<T>(top_bits, Larger(), lds, turn));
+            s = scale_from(over_row<T>(__builtin_bit_cast(uint32_t, top) & 0x7FFFFFFFu, Larger(), lds, turn));
             if (!r.exact || s.tiny) {
                 const float near = s.tiny ? 0.0f : (float)s.top * kNearTop;
                 double t = 0.0;
-                for (int c = threadIdx.x; c < a.C && s.fine; c += T) {
-                    const float v = r.value(c, false);
-                    if (fabsf(r.z32(c, v)) >= near) t = Larger()(t, fabs(r.z64(c, v)));
-                }
+                if (s.fine && top >= near)
+                    for (int c = threadIdx.x * V; c < a.C; c += T * V)
+#pragma unroll 1
+                        for (int at = c; at < min(c + V, a.C); ++at) {
+                            const float value = r.value(at, false);
+                            if (fabsf(r.z32(at, value)) >= near) t = Larger()(t, fabs(r.z64(at, value)));
+                        }
                 t = over_row<T>(t, Larger(), lds, turn);
                 if (s.fine) s.top = t;
             }
             s.reach = s.top > 0.0 ? 127.0f / (float)s.top : 0.0f;
         }
         int total = 0;
-        for (int c = threadIdx.x; c < a.C; c += T) {
-            const float v = r.value(c, false);
-            const float z = r.z32(c, v);
-            if (is_norm(MODE) && r.h) r.h[c] = E::from_f32(v);
+        for (int c = threadIdx.x * V; c < a.C; c += T * V) {
+            const int n = a.C - c;
+            piece(c, n, v, z);
+            if (is_norm(MODE) && r.h) store_words<E>(r.h + c, rounded<E>(v), n);
             if (MODE == kNorm) {
-                r.y[c] = E::from_f32(z * factor);
-            } else {
-                const float t = z * s.reach;
-                float q = rintf(t);
-                if (s.fine && s.top > 0.0 && (s.tiny || fabsf(t - q) > 0.5f - r.margin(t))) q = (float)rint(127.0 * r.z64(c, v) / s.top);
-                const int code = s.fine ? (int)q : 0;
-                r.codes[c] = (int8_t)code;
-                total += code;
+#pragma unroll
+                for (int e = 0; e < V; ++e) z[e] *= factor;
+                store_words<E>(r.y + c, rounded<E>(z), n);
+                continue;
             }
+            uint32_t near = 0;
+            Piece<Code, V> o;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float t = z[e] * s.reach, q = rintf(t);
+                near |= (s.tiny || fabsf(t - q) > 0.5f - r.margin(t) ? 1u : 0u) << e;
+                o.e[e] = s.fine ? (int8_t)(int)q : 0;
+                total += o.e[e];
+            }
+            store_piece<Code, V>(r.codes + c, o, n);
+            if (s.fine && s.top > 0.0)
+                for (; near; near &= near - 1) {
+                    const int at = c + __builtin_ctz(near);
+                    if (at >= a.C) break;
+                    const int code = (int)rint(127.0 * r.z64(at, r.value(at, true)) / s.top);
+                    total += code - r.codes[at];
+                    r.codes[at] = (int8_t)code;
+                }
         }
         if (MODE != kNorm) {
             if (a.rowsum) {
@@ -435,7 +473,8 @@ int launch_held(const RowArgs &a, hipStream_t stream) {
     using std::integral_constant;
     // As few threads as hold the row in registers, up to 8 pieces each: no exchange through LDS up to 256 pieces, and more rows at once on a
     // compute unit.  32760 x 8960 bf16 with 256 threads of 5 pieces against 512 of 3, us: norm 203 and 199, its codes 163 and 216, quant8 179 and 188,
-    // gated 323 and 424; 32760 x 13824 fp32 with 512 threads of 8 against 1024 of 4: 617 and 622, 509 and 669, 392 and 390, 835 and 915.
+    // gated 323 and 424; 32760 x 13824 fp32 with 512 threads of 8 against 1024 of 4: 617 and 622, 509 and 669, 392 and 390, 835 and 915;
+    // 3000 x 30000 bf16 74 and 72, 83 and 73, 81 and 69, 146 and 130.  Longer rows are read again: 3000 x 30000 fp32 187, 227, 138, 358.
     if (pieces <= 8) return launch(integral_constant<int, 8>(), integral_constant<int, 1>());
     if (pieces <= 16) return launch(integral_constant<int, 16>(), integral_constant<int, 1>());
     if (pieces <= 32) return launch(integral_constant<int, 32>(), integral_constant<int, 1>());
@@ -451,9 +490,12 @@ int launch_held(const RowArgs &a, hipStream_t stream) {
     if (pieces <= 1280) return launch(four, integral_constant<int, 5>());
     if (pieces <= 1536) return launch(four, integral_constant<int, 6>());
     if (pieces <= 2048) return launch(four, integral_constant<int, 8>());
-    const integral_constant<int, 512> eight;
-    if (pieces <= 3072) return launch(eight, integral_constant<int, 6>());
-    if (pieces <= 4096) return launch(eight, integral_constant<int, 8>());
+    if constexpr (E::kVec == 8) {
+        if (pieces <= 4096) return launch(integral_constant<int, 1024>(), integral_constant<int, 4>());
+    } else {
+        if (pieces <= 3072) return launch(integral_constant<int, 512>(), integral_constant<int, 6>());
+        if (pieces <= 4096) return launch(integral_constant<int, 512>(), integral_constant<int, 8>());
+    }
     row_long<E, MODE><<<dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), 1024, 0, stream>>>(a);
     return check_launch();
 }
