@@ -299,6 +299,6 @@ const char *dvdq_status_string(int status) {
     }
 }
 
-int dvdq_version(void) { return 230; }
+int dvdq_version(void) { return 240; }
 
 }  // extern "C"

@@ -38,7 +38,8 @@ struct Op8 {                           // 8-bit codes, exact sums, a scale per t
     using Out = E;
     using Acc = v4i;
     static constexpr bool kScaled = true;
-    static constexpr int kBytes = 1;    static __device__ __forceinline__ v4i mfma(uint4 a, uint4 b, v4i c) {
+    static constexpr int kBytes = 1;
+    static __device__ __forceinline__ v4i mfma(uint4 a, uint4 b, v4i c) {
         return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(v4i, a), __builtin_bit_cast(v4i, b), c, 0, 0, 0);
     }
 };
@@ -481,9 +482,11 @@ __device__ uint4 zero_piece;   // what the pieces past K of the last slice are r
 
 // Tiles of 64 WN channels x 16 FM WM tokens, WN x WM waves of 64 channels x 16 FM tokens each; slices of 128 bytes of K.
 // Tokens have three slices in LDS, weights two: while a slice is multiplied, the next is there, the tokens of the one after it
-// come in, and its weights follow as soon as those of the present slice have been read.  (The tokens are what comes from further away; with
-// three slices of weights in place of tokens 8-bit 32760 x 13824 x 5120 took 1734 to 1810 us in place of 1693 to 1757, 32760 x 8960 x 1536 360 in place of 351.)  (What bounds the loop on a full chip is the way from
-// the L2s into LDS, 54 to 69 GB/s per compute unit where 32 of them share panels; it must not run dry.)
+// come in, and its weights follow as soon as those of the present slice have been read.  (The tokens are what comes from further away: with three
+// slices of weights and two of tokens 8-bit 32760 x 13824 x 5120 took 1734 to 1810 us in place of 1693 to 1757, 32760 x 8960 x 1536 360 in place of 351.
+// What bounds the loop on a full chip is the way from the L2s into LDS, 54 to 69 GB/s per compute unit where 32 of them share panels; it must not run dry.
+// Five slices of tokens and four of weights for 128 x 128 and smaller tiles: 8-bit 600 x 4608 x 1536 20.1 -> 16.0 us, 17 x 13824 x 5120 23.7 -> 20.3, 1000 x 8960 x 1536
+// 28.1 -> 25.6, but 1560 x 1536 x 1536 11.3 -> 11.9, 512 x 4096 x 5120 level, and one workgroup a compute unit; not kept.)
 // A slice is worked off in phases of 16 matrix instructions (or fewer), and a phase begins by requesting the fragments of the next one.
 // Before the last phase of a slice, whose fragments are then in registers, stands the slice's one barrier: behind it the next slice is
 // in LDS for every wave, and this one's place is free.
@@ -672,7 +675,8 @@ struct LinearPlan { int shape, splits, slices, group_n; size_t parts_bytes, pad_
 // compute unit for itself and nothing hides its outputs.  Parts of K are written and read back at 9.2 TB/s (they stay in the caches), by a
 // launch of 3.2 us.  The constants are fitted to 818 timings of 67 outputs (32 to 118800 tokens, 64 to 11384 channels, K 64 to 13824) with every shape
 // and 1 to 12 parts: the choice takes 2 % longer than the best of them in the mean, 13 % at most; always 128 x 128 without parts
-// 35 % in the mean, 6.2 times at most.
+// 35 % in the mean, 6.2 times at most.  8-bit codes, whose slices have as many bytes and matrix instructions: at 15 sizes 4 % longer than the best in the mean,
+// 15 % at most (17 x 13824 x 5120, 600 x 4608 x 1536).
 // K: bytes of a row
 inline LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
     const int total = (int)((K + 127) / 128);
@@ -735,7 +739,6 @@ int launch_product(const LinearArgs &a, const LinearPlan &p, bool any, hipStream
         default: return launch_tiles<P, ACT, 2, 1, 2>(a, 4, p.group_n, stream);
     }
 }
-
 
 // addresses and pitches of an operand that tiles read straight into LDS
 inline bool whole_pieces(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 15) == 0 && ld < (int64_t)1 << 23; }
