@@ -93,6 +93,8 @@ int dvdq_bench_set_gbs_wait(int64_t ticks);
  * they go through registers.  Host only.
  */
 int dvdq_bench_linear_choice(int64_t M, int64_t N, int64_t K, int any);
+/* The same for dvdq_linear8 (whose pieces are 16 codes). */
+int dvdq_bench_linear8_choice(int64_t M, int64_t N, int64_t K, int any);
 
 #ifdef __cplusplus
 }

@@ -41,7 +41,7 @@ EXPORTED_SYMBOLS = (
     "dvdq_qlinear_scale_offset", "dvdq_qlinear_rowsum_offset", "dvdq_qlinear_static", "dvdq_static_workspace_bytes", "dvdq_w4_prepack", "dvdq_w4_native_bytes", "dvdq_w4_prepack_fp6",
     "dvdq_w4_native_fp6_bytes", "dvdq_codes_bytes", "dvdq_status_string",
     "dvdq_version", "dvdq_rope", "dvdq_rope_table", "dvdq_linear", "dvdq_linear_workspace_bytes", "dvdq_bench_linear_choice", "dvdq_group_norm", "dvdq_group_norm_workspace_bytes",
-    "dvdq_rms_norm", "dvdq_rms_norm_quant", "dvdq_quant8", "dvdq_linear8", "dvdq_linear8_workspace_bytes",
+    "dvdq_rms_norm", "dvdq_rms_norm_quant", "dvdq_quant8", "dvdq_linear8", "dvdq_linear8_workspace_bytes", "dvdq_bench_linear8_choice",
     "dvdq_gbs_workspace_bytes", "dvdq_gbs_reset", "dvdq_gbs_step", "dvdq_bgr_quantize", "dvdq_bench_copy", "dvdq_bench_mfma_i8", "dvdq_bench_mfma_fp6", "dvdq_bench_set_gemm_variant", "dvdq_bench_set_gemm_schedule", "dvdq_bench_fill_tile_counters", "dvdq_bench_set_gemm_grid_limit", "dvdq_bench_set_gbs_wait", "dvdq_bench_gemm_choice", "dvdq_bench_narrow_tiles", "dvdq_bench_quantizer_waves", "dvdq_bench_qlinear_choice", "dvdq_bench_bgr_choice", "dvdq_release_stream",
 )
 
@@ -162,6 +162,8 @@ def lib() -> C.CDLL:
     L.dvdq_linear8.restype = i32
     L.dvdq_linear8_workspace_bytes.argtypes = [i64, i64, i64]
     L.dvdq_linear8_workspace_bytes.restype = sz
+    L.dvdq_bench_linear8_choice.argtypes = [i64, i64, i64, i32]
+    L.dvdq_bench_linear8_choice.restype = i32
     L.dvdq_bench_copy.argtypes = [vp, vp, sz, vp]
     L.dvdq_bench_mfma_i8.argtypes = [i32, i32, vp, C.POINTER(C.c_double), vp]
     L.dvdq_bench_mfma_fp6.argtypes = [i32, i32, vp, C.POINTER(C.c_double), vp]
@@ -1013,6 +1015,11 @@ def bench_qlinear_choice(M: int, N: int, K: int, x: int = 1 << 40, y: int = 1 <<
 def bench_linear_choice(M: int, N: int, K: int, any: bool = False) -> int:
     """How linear takes a product (see dvdq_bench_linear_choice).  Needs no GPU."""
     return lib().dvdq_bench_linear_choice(M, N, K, int(any))
+
+
+def bench_linear8_choice(M: int, N: int, K: int, any: bool = False) -> int:
+    """How linear8 takes a product (see dvdq_bench_linear8_choice).  Needs no GPU."""
+    return lib().dvdq_bench_linear8_choice(M, N, K, int(any))
 
 
 def bench_set_gemm_schedule(schedule: int) -> None:

@@ -198,6 +198,11 @@ size_t dvdq_linear8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     return dvdq::linear8_workspace_bytes(M, N, K);
 }
 
+int dvdq_bench_linear8_choice(int64_t M, int64_t N, int64_t K, int any) {
+    if (M < 1 || N < 1 || K < 1 || M > kMaxTokens || N > kMaxChannels || K > kMaxCodeK) return -2;
+    return dvdq::linear8_choice(M, N, K, any || K % 16 != 0);
+}
+
 int dvdq_linear8(const int8_t *codes, int64_t ldc, const float *x_scale, const int8_t *w, int64_t ldw, const float *w_scale, const void *bias, int act,
                  const void *gate, int64_t gate_rows, int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype,
                  void *y, int64_t ldy, void *workspace, size_t workspace_bytes, void *hip_stream) {

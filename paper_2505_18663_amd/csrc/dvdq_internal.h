@@ -182,6 +182,7 @@ int launch_rms_norm(const void *x, int64_t B, int64_t S, int64_t C, int64_t x_ba
 int launch_quant8(const void *x, int64_t ldx, const void *up, int64_t ldu, int act, int64_t M, int64_t C, int dtype, int8_t *codes, int64_t ldc,
                   float *x_scale, int32_t *code_rowsum, hipStream_t stream);
 size_t linear8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int linear8_choice(int64_t M, int64_t N, int64_t K, bool any);
 int launch_linear8(const int8_t *codes, int64_t ldc, const float *x_scale, const int8_t *w, int64_t ldw, const float *w_scale, const void *bias, int act,
                    const void *gate, int64_t gate_rows, int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype,
                    void *y, int64_t ldy, void *workspace, hipStream_t stream);

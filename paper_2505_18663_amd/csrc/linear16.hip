@@ -14,11 +14,7 @@ namespace dvdq {
 
 size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K) { return workspace_for(M, N, 2 * K, false); }
 
-int linear_choice(int64_t M, int64_t N, int64_t K, bool any) {
-    if (few_tokens(M, N, 2 * K, false)) return -1;
-    const LinearPlan p = linear_plan(M, N, 2 * K, any);
-    return p.shape + 16 * p.splits + (p.pad_bytes ? 4096 : any ? 8192 : 0);
-}
+int linear_choice(int64_t M, int64_t N, int64_t K, bool any) { return choice_for(M, N, 2 * K, any, false); }
 
 int launch_linear(const void *x, int64_t ldx, const void *w, int64_t ldw, const void *bias, int act, const void *gate, int64_t gate_rows,
                   int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype, void *y, int64_t ldy,

@@ -15,6 +15,8 @@ namespace dvdq {
 
 size_t linear8_workspace_bytes(int64_t M, int64_t N, int64_t K) { return workspace_for(M, N, K, true); }
 
+int linear8_choice(int64_t M, int64_t N, int64_t K, bool any) { return choice_for(M, N, K, any, true); }
+
 int launch_linear8(const int8_t *codes, int64_t ldc, const float *x_scale, const int8_t *w, int64_t ldw, const float *w_scale, const void *bias, int act,
                    const void *gate, int64_t gate_rows, int64_t ldg, const void *residual, int64_t ldr, int64_t M, int64_t N, int64_t K, int dtype,
                    void *y, int64_t ldy, void *workspace, hipStream_t stream) {

@@ -280,57 +280,63 @@ static __device__ __forceinline__ void store_part(const LinearArgs &a, const Acc
         for (int i = 0; i < 4; ++i) a.parts[((at + j) * 4 + i) * 64 + (threadIdx.x & 63)] = __builtin_bit_cast(float4, acc[i][j]);
 }
 
-// Any sizes, pitches and addresses: 128 x 128 outputs of four waves, 64 x 64 each, operands through registers into LDS rows of 128
-// bytes of K, a slice ahead.  LDS as in linear_tiles.
-template <typename P, int ACT>
-__global__ __launch_bounds__(256, 2) void linear_any(LinearArgs a) {
-    extern __shared__ uint4 lds[];                           // two slices of 128 rows of weights, 128 of tokens
+// Any sizes, pitches and addresses: tiles as in linear_tiles, a workgroup each, operands through registers into LDS rows of 128 bytes of K, a
+// slice ahead.  LDS as there.
+template <typename P, int ACT, int FM, int WN, int WM>
+__global__ __launch_bounds__(64 * WN * WM, 2) void linear_any(LinearArgs a, int group_n) {
+    constexpr int W = WN * WM, BN = 64 * WN, BM = 16 * FM * WM, R = 8 * W;   // R: rows that the threads have a piece each of
+    constexpr int LW = BN / R, LX = BM / R;
+    extern __shared__ uint4 lds[];                           // two slices of BN rows of weights, BM of tokens
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n_tiles = (a.N + 127) / 128, m_tiles = (a.M + 127) / 128, tiles = n_tiles * m_tiles;
-    const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
-    const int tile_m = tile / n_tiles;
-    const int n0 = (tile - tile_m * n_tiles) * 128, m0 = tile_m * 128;
-    const int wn = (wave & 1) * 64, wm = (wave >> 1) * 64;
+    const int n_tiles = (a.N + BN - 1) / BN, m_tiles = (a.M + BM - 1) / BM, tiles = n_tiles * m_tiles, grid = gridDim.x;
+    const int xcds = min(8, grid), xcd = blockIdx.x % xcds, share = grid / xcds, more = grid % xcds;   // (a run of tiles for each XCD, as there)
+    const int t = share * xcd + min(xcd, more) + blockIdx.x / xcds, split = t / tiles;
+    int m0, n0;
+    tile_origin(t - split * tiles, m_tiles, n_tiles, group_n, BM, BN, m0, n0);
+    const int wn = wave % WN * 64, wm = wave / WN * 16 * FM;
     const int q0 = split * a.slices, q1 = min(q0 + a.slices, (a.K + 127) >> 7);
-    typename P::Acc acc[4][4] = {};
+    typename P::Acc acc[4][FM] = {};
     const int piece = tid & 7, row0 = tid >> 3;
-    uint4 pw[4], px[4];
-    auto load = [&](int q) {
-        const int k = q * 128 + piece * 16, count = min(16, a.K - k);
+    uint4 pw[LW], px[LX];
+    auto load = [&](int q, auto whole) __attribute__((always_inline)) {   // whole: the slice lies within the rows
+        constexpr bool WHOLE = decltype(whole)::value;
+        const int k = q * 128 + piece * 16, count = WHOLE ? 16 : min(16, a.K - k);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = row0 + 32 * i;
-            pw[i] = load_operand<P>(a.w + min(n0 + channel_of_row(row), a.N - 1) * a.ldw + k, count, a.K);
-            px[i] = load_operand<P>(a.x + min(m0 + row, a.M - 1) * a.ldx + k, count, a.K);
-        }
+        for (int i = 0; i < LW; ++i) pw[i] = load_operand<P>(a.w + min(n0 + channel_of_row(row0 + R * i), a.N - 1) * a.ldw + k, count, a.K);
+#pragma unroll
+        for (int i = 0; i < LX; ++i) px[i] = load_operand<P>(a.x + min(m0 + row0 + R * i, a.M - 1) * a.ldx + k, count, a.K);
     };
-    if (q0 < q1) load(q0);
+    if (q0 < q1) load(q0, std::false_type());
     for (int q = q0; q < q1; ++q) {
-        uint4 *lds_w = lds + (q & 1) * 2048, *lds_x = lds_w + 1024;
+        uint4 *lds_w = lds + (q & 1) * (8 * (BN + BM)), *lds_x = lds_w + 8 * BN;
+        const int at = row0 * 8 + (piece ^ ((row0 >> 1) & 7));   // (R is a multiple of 16: the same exchange of pieces in all of a thread's rows)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = row0 + 32 * i, at = row * 8 + (piece ^ ((row >> 1) & 7));
-            lds_w[at] = pw[i];
-            lds_x[at] = px[i];
-        }
+        for (int i = 0; i < LW; ++i) lds_w[at + 8 * R * i] = pw[i];
+#pragma unroll
+        for (int i = 0; i < LX; ++i) lds_x[at + 8 * R * i] = px[i];
         __syncthreads();                                     // (and every wave has read the slice before the last)
-        if (q + 1 < q1) load(q + 1);
+        if ((q + 2) * 128 <= a.K && q + 1 < q1) load(q + 1, std::true_type());
+        else if (q + 1 < q1) load(q + 1, std::false_type());
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            uint4 fw[4], fx[4];
+            uint4 fw[4], fx[FM];
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
-                const int rw = wn + 16 * f + (lane & 15), rx = wm + 16 * f + (lane & 15), p = 4 * ks + (lane >> 4);
+                const int rw = wn + 16 * f + (lane & 15), p = 4 * ks + (lane >> 4);
                 fw[f] = lds_w[rw * 8 + (p ^ ((rw >> 1) & 7))];
+            }
+#pragma unroll
+            for (int f = 0; f < FM; ++f) {
+                const int rx = wm + 16 * f + (lane & 15), p = 4 * ks + (lane >> 4);
                 fx[f] = lds_x[rx * 8 + (p ^ ((rx >> 1) & 7))];
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = P::mfma(fw[i], fx[j], acc[i][j]);
+                for (int j = 0; j < FM; ++j) acc[i][j] = P::mfma(fw[i], fx[j], acc[i][j]);
         }
     }
-    if constexpr (ACT == kPart) store_part(a, acc, ((int64_t)blockIdx.x * 4 + wave) * 4);
+    if constexpr (ACT == kPart) store_part(a, acc, ((int64_t)t * W + wave) * FM);
     else epilogue<P, ACT>(a, acc, __builtin_amdgcn_readfirstlane(m0 + wm), __builtin_amdgcn_readfirstlane(n0 + wn));
 }
 
@@ -664,7 +670,7 @@ int launch_tiles(const LinearArgs &a, int per_cu, int group_n, hipStream_t strea
 // The shapes of tiles: channels, tokens, workgroups per compute unit (LDS)
 struct Shape { int fm, wn, wm, per_cu; };
 constexpr Shape kShapes[] = {{8, 4, 2, 1}, {4, 4, 2, 1}, {4, 2, 2, 2}, {2, 2, 2, 2}, {2, 1, 2, 4}};
-constexpr int kShapeAny = 2;   // linear_any's
+constexpr int kShapeAny = 2;   // linear_any's; for codes it has the smallest too
 
 struct LinearPlan { int shape, splits, slices, group_n; size_t parts_bytes, pad_bytes; float time; };
 
@@ -677,14 +683,19 @@ struct LinearPlan { int shape, splits, slices, group_n; size_t parts_bytes, pad_
 // and 1 to 12 parts: the choice takes 2 % longer than the best of them in the mean, 13 % at most; always 128 x 128 without parts
 // 35 % in the mean, 6.2 times at most.  8-bit codes, whose slices have as many bytes and matrix instructions: at 15 sizes 4 % longer than the best in the mean,
 // 15 % at most (17 x 13824 x 5120, 600 x 4608 x 1536).
-// K: bytes of a row
-inline LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
+// Through registers: 16-bit products, 1.7 times that.  8-bit ones, a slice alone 0.3 us and 1.2 per 64 KB, or 1.5 times the share of the loads: of 15 sizes
+// with rows that are no whole pieces (40 to 50000 tokens, 100 to 12000 channels, K 88 to 9001) the choice, copies among it, takes 0.4 % longer than
+// the best of them in the mean, 5 % at most.  us, 128 x 128 tiles, 64 x 64, copied: 6242 x 1160 x 1156 20.5, 30.2, 26.4; 188 x 1720 x 1376 17.9, 13.8
+// (11.3 in parts), 14.1; 40 x 9001 x 1000 93, 62 (15.8 in parts), 20.1; 50000 x 777 x 100 20.9, 30.9, 30.9; 22268 x 4824 x 752 161, 215, 125;
+// 10000 x 5000 x 5120 362, 544, 279.
+// K: bytes of a row; codes: 8-bit ones
+inline LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any, bool codes) {
     const int total = (int)((K + 127) / 128);
     const bool lines = K % 128 == 0;
     LinearPlan best = {};
     best.time = 1e30f;
     for (int i = 0; i < (int)(sizeof(kShapes) / sizeof(kShapes[0])); ++i) {
-        if (any && i != kShapeAny) continue;
+        if (any && i != kShapeAny && !(codes && i == 4)) continue;
         const Shape &sh = kShapes[i];
         const int bn = 64 * sh.wn, bm = 16 * sh.fm * sh.wm, n_tiles = (int)((N + bn - 1) / bn), slots = 256 * sh.per_cu;
         const int64_t tiles = n_tiles * ((M + bm - 1) / bm);
@@ -694,18 +705,19 @@ inline LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
             if (want > 1 && (per < 4 || splits == 1 || tiles * splits > slots)) break;
             const int64_t items = tiles * splits, full = items / slots;
             const int rest = (int)(items - full * slots);
-            const float load = bytes * (lines ? 1.0f : 1.15f) * (1 / 275e3f + (items < 256 ? (float)items / 256 : 1.0f) / 100e3f);
-            const float lone = 0.34f + (lines ? 0.23f : 0.43f) / 65536 * bytes;
+            const bool held = any && codes;                  // (on the way to LDS in registers)
+            const float load = bytes * (lines ? 1.0f : 1.15f) * (held ? 1.5f : 1.0f) * (1 / 275e3f + (items < 256 ? (float)items / 256 : 1.0f) / 100e3f);
+            const float lone = held ? 0.3f + 1.2f / 65536 * bytes : 0.34f + (lines ? 0.23f : 0.43f) / 65536 * bytes;
             auto round = [&](int resident) {
                 return 1.6f + (0.4f * (float)resident + (sh.per_cu == 1 ? 5.7f : 0.0f)) * area +
                        (float)per * (std::max(lone, (float)resident * std::max(load, 1.19f * area)) + 0.1f * (float)resident * area);
             };
             float time = (float)full * round(sh.per_cu) + (rest ? round((rest + 255) / 256) : 0.0f);
             if (splits > 1) time += 3.2f + (float)items * area * (8 * 65536 / 9.2e6f);
-            if (any) time *= 1.7f;
+            if (any && !codes) time *= 1.7f;
             if (time < best.time) {
                 const int groups = (n_tiles + 5) / 6;   // columns of tiles that are run through before the next row
-                best = {i, splits, per, any ? n_tiles : (n_tiles + groups - 1) / groups, splits > 1 ? (size_t)(items * bn * bm) * sizeof(float) : 0, 0, time};
+                best = {i, splits, per, any && !codes ? n_tiles : (n_tiles + groups - 1) / groups, splits > 1 ? (size_t)(items * bn * bm) * sizeof(float) : 0, 0, time};
             }
         }
     }
@@ -713,7 +725,7 @@ inline LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
     // LDS cost it 1.4 to 1.9 times the time of 128 x 128 tiles: 32760 x 1533 x 8960 1388 us, copied 780).
     if (any && K % 16 != 0) {
         const int64_t pitch = (K + 127) / 128 * 128;
-        LinearPlan p = linear_plan(M, N, pitch, false);
+        LinearPlan p = linear_plan(M, N, pitch, false, codes);
         p.pad_bytes = (size_t)((M + N) * pitch);
         p.time += 3.0f + (float)p.pad_bytes * (2 / 5e6f);
         if (p.time < best.time) return p;
@@ -722,14 +734,24 @@ inline LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any) {
 }
 inline size_t plan_bytes(const LinearPlan &p) { return (p.pad_bytes + 255) / 256 * 256 + p.parts_bytes; }
 
+template <typename P, int ACT, int FM, int WN, int WM>
+int launch_any(const LinearArgs &a, int group_n, hipStream_t stream) {
+    constexpr int BN = 64 * WN, BM = 16 * FM * WM;
+    constexpr size_t kLds = 2 * (BN + BM) * 128;
+    static std::atomic<uint64_t> done{0};
+    const auto kernel = linear_any<P, ACT, FM, WN, WM>;
+    allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kLds, done);
+    kernel<<<dim3((unsigned)(((a.N + BN - 1) / BN) * ((a.M + BM - 1) / BM) * a.splits)), 64 * WN * WM, kLds, stream>>>(a, group_n);
+    return check_launch();
+}
+
 template <typename P, int ACT>
 int launch_product(const LinearArgs &a, const LinearPlan &p, bool any, hipStream_t stream) {
     if (any) {
-        static std::atomic<uint64_t> done{0};
-        constexpr size_t kLds = 2 * 256 * 128;
-        allow_dynamic_lds(reinterpret_cast<const void *>(linear_any<P, ACT>), kLds, done);
-        linear_any<P, ACT><<<dim3((unsigned)(((a.N + 127) / 128) * ((a.M + 127) / 128) * a.splits)), 256, kLds, stream>>>(a);
-        return check_launch();
+        if constexpr (P::kScaled) {
+            if (p.shape == 4) return launch_any<P, ACT, 2, 1, 2>(a, p.group_n, stream);
+        }
+        return launch_any<P, ACT, 4, 2, 2>(a, p.group_n, stream);
     }
     switch (p.shape) {
         case 0: return launch_tiles<P, ACT, 8, 4, 2>(a, 1, p.group_n, stream);
@@ -743,10 +765,17 @@ int launch_product(const LinearArgs &a, const LinearPlan &p, bool any, hipStream
 // addresses and pitches of an operand that tiles read straight into LDS
 inline bool whole_pieces(const void *p, int64_t ld) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && (ld & 15) == 0 && ld < (int64_t)1 << 23; }
 
+// see dvdq_bench_linear_choice
+inline int choice_for(int64_t M, int64_t N, int64_t K, bool any, bool codes) {
+    if (few_tokens(M, N, K, codes)) return -1;
+    const LinearPlan p = linear_plan(M, N, K, any, codes);
+    return p.shape + 16 * p.splits + (p.pad_bytes ? 4096 : any ? 8192 : 0);
+}
+
 inline size_t workspace_for(int64_t M, int64_t N, int64_t K, bool codes) {
     if (few_tokens(M, N, K, codes)) return 0;
-    const size_t any = plan_bytes(linear_plan(M, N, K, true));   // (addresses and pitches are not known here)
-    return K % 16 == 0 ? std::max(any, plan_bytes(linear_plan(M, N, K, false))) : any;
+    const size_t any = plan_bytes(linear_plan(M, N, K, true, codes));   // (addresses and pitches are not known here)
+    return K % 16 == 0 ? std::max(any, plan_bytes(linear_plan(M, N, K, false, codes))) : any;
 }
 
 // The product of operands P; those of the output's type come into play in the last of the launches only.
@@ -757,7 +786,7 @@ int launch_few_or_tiles(LinearArgs a, void *workspace, hipStream_t stream) {
         return check_launch();
     }
     bool any = a.K % 16 != 0 || !whole_pieces(a.x, a.M > 1 ? a.ldx : 0) || !whole_pieces(a.w, a.N > 1 ? a.ldw : 0);
-    const LinearPlan p = linear_plan(a.M, a.N, a.K, any);
+    const LinearPlan p = linear_plan(a.M, a.N, a.K, any, P::kScaled);
     a.parts = reinterpret_cast<float4 *>(static_cast<uint8_t *>(workspace) + (p.pad_bytes + 255) / 256 * 256);
     if (p.pad_bytes) {
         const int pitch = (a.K + 127) / 128 * 128;

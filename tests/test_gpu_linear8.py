@@ -60,8 +60,7 @@ def test_sizes(size, dtype):
     check(args, f"{size} all", on, dtype=dtype, bias=tensor(g, N, dtype=dtype), act=dvdq.ACT_GELU_TANH, gate=gate, residual=tensor(g, M, N, dtype=dtype))
 
 
-# a size for each shape of tile (0: 256 x 256 .. 4: 64 x 64), whole and in parts of K: which one a size takes is that of the 16-bit product with as many bytes
-# in a row (see test_rows8_linear8.py)
+# a size for each shape of tile (0: 256 x 256 .. 4: 64 x 64), whole and in parts of K (see test_rows8_linear8.py)
 WAYS = {(0, 1): (2600, 5120, 784), (0, 3): (2600, 1540, 13824), (1, 1): (12000, 260, 1168), (1, 4): (6200, 136, 8208), (2, 1): (12000, 136, 48),
         (2, 11): (70, 1540, 8208), (3, 1): (70, 9000, 48), (3, 7): (70, 1540, 4112), (4, 1): (40, 48, 48), (4, 4): (40, 48, 2064)}
 
@@ -75,6 +74,23 @@ def test_every_shape_of_tile(way, dtype):
     bias, gate, residual = tensor(g, N, dtype=dtype), tensor(g, 2, N, dtype=dtype), tensor(g, M, N, dtype=dtype)
     for kw in ({}, {"gate": gate}, {"residual": residual}, {"gate": gate, "residual": residual, "act": dvdq.ACT_SILU}, {"gate": residual, "residual": residual}):
         check(args, f"{way} {dtype} {list(kw)}", DEV, dtype=dtype, bias=bias, **kw)
+
+
+# rows that are no whole pieces: through registers as 128 x 128 and 64 x 64 tiles, whole and in parts, and copied first
+ROWS = [(6242, 1160, 1156), (2000, 500, 1000), (417, 200, 136), (188, 1376, 1720), (100, 3000, 3001), (40, 1000, 9001), (2600, 5120, 777), (600, 2000, 4001), (70, 130, 100)]
+
+
+@pytest.mark.parametrize("size", ROWS)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_that_are_no_whole_pieces(size, dtype):
+    M, N, K = size
+    g = gen(K)
+    args = operands(g, M, N, K)
+    check(args, f"{size} {dtype}", DEV, dtype=dtype)
+    check(args, f"{size} {dtype} all", DEV, dtype=dtype, bias=tensor(g, N, dtype=dtype), act=dvdq.ACT_GELU, gate=tensor(g, N, dtype=dtype), residual=tensor(g, M, N, dtype=dtype))
+    # whole pieces at an address that is none
+    x, w = ints(g, M, K + 40)[:, 8:8 + K // 16 * 16], ints(g, N, K + 25)[:, 1:1 + K // 16 * 16]
+    check((x, args[1], w, args[3]), f"{size} {dtype} address", DEV, dtype=dtype, residual=tensor(g, M, N, dtype=dtype))
 
 
 @pytest.mark.parametrize("M", [3, 40, 700])

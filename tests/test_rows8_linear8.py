@@ -85,21 +85,27 @@ def test_the_binding_refuses_what_is_not_on_a_gpu():
 def test_the_sizes_that_stand_for_each_shape_of_tile_take_it():
     from test_gpu_linear8 import WAYS
     for (shape, parts), (M, N, K) in WAYS.items():
-        assert dvdq.bench_linear_choice(M, N, K // 2) == shape + 16 * parts, (M, N, K)
+        assert dvdq.bench_linear8_choice(M, N, K) == shape + 16 * parts, (M, N, K)
         bn, bm = {0: (256, 256), 1: (256, 128), 2: (128, 128), 3: (128, 64), 4: (64, 64)}[shape]
         need = -(-M // bm) * -(-N // bn) * parts * bm * bn * 4 if parts > 1 else 0
         assert dvdq.linear8_workspace_bytes(M, N, K) >= need
     assert {shape for shape, _ in WAYS} == set(range(5))
-    assert dvdq.linear8_workspace_bytes(8, 5120, 13824) == 0 and dvdq.linear8_workspace_bytes(16, 5120, 5120) == 0    # few tokens: straight from the weights
+    for M, N, K in ((8, 5120, 13824), (16, 5120, 5120)):    # few tokens: straight from the weights
+        assert dvdq.bench_linear8_choice(M, N, K) == dvdq.bench_linear8_choice(M, N, K, True) == -1 and dvdq.linear8_workspace_bytes(M, N, K) == 0
 
 
 def test_the_workspace_holds_whatever_way_the_addresses_ask_for():
     """Rows that are no whole pieces are copied, or read through registers, in parts of K: the size is for the larger."""
-    for M, N, K in ((40, 48, 1168), (600, 5120, 4001), (33, 65, 1000), (300, 77, 5000)):
+    from test_gpu_linear8 import ROWS
+    ways = set()
+    for M, N, K in (*ROWS, (40, 48, 1168), (33, 65, 1000)):
         for any_ in (False, True):
-            c = dvdq.bench_linear_choice(M, N, (K + 1) // 2, any_ or K % 16 != 0)
+            c = dvdq.bench_linear8_choice(M, N, K, any_)
+            assert c == dvdq.bench_linear8_choice(M, N, K, any_)
+            ways.add((c % 16, min(c // 16 % 256, 2), c >> 12))
             shape, parts, pad = c % 16, c // 16 % 256, bool(c & 4096)
             bn, bm = {0: (256, 256), 1: (256, 128), 2: (128, 128), 3: (128, 64), 4: (64, 64)}[shape]
             need = -(-M // bm) * -(-N // bn) * parts * bm * bn * 4 if parts > 1 else 0
             need += (M + N) * (-(-K // 128) * 128) if pad else 0
             assert dvdq.linear8_workspace_bytes(M, N, K) >= need, (M, N, K)
+    assert {(2, 1, 2), (4, 1, 2), (4, 2, 2)} <= ways and any(w[2] == 1 for w in ways)    # through registers as both tiles, whole and in parts; copied
