@@ -211,3 +211,21 @@ def test_a_run_of_them_together():
     # and codes of the rotating quantizer here
     codes, scale = dvdq.rotate_quant(h, 1, 8)
     assert_close(dvdq.linear8(codes, scale, c1, s1), *linear8_64(codes, scale, c1, s1), "rotate_quant")
+
+
+@pytest.mark.parametrize("size", [(420000, 5200, 64), (420000, 5200, 72), (40000, 64, 131056), (40000, 64, 131071), (40000, 1000, 131071)])
+def test_beyond_32_bits_of_elements(size):
+    """Outputs of more than 2^31 elements, codes of more than 2^32 bytes: straight, copied and through registers."""
+    M, N, K = size
+    g = gen(9)
+    codes = torch.empty((M, K), dtype=torch.int8, device=DEV).random_(-127, 128, generator=g)
+    _, xs, w, ws = operands(g, 1, N, K)
+    xs = torch.exp(tensor(g, M, scale=0.3)) / 127
+    y = torch.ones((M, N), dtype=torch.bfloat16, device=DEV)
+    gate = tensor(g, N, dtype=torch.bfloat16)
+    assert dvdq.linear8(codes, xs, w, ws, gate=gate, residual=y, y=y) is y
+    for first in (0, M // 2 - 3, (1 << 31) // N - 3, (1 << 32) // K - 3, M - 50):
+        if 0 <= first < M:
+            part = slice(first, min(first + 50, M))
+            ref, slack = linear8_64(codes[part], xs[part], w, ws, gate=gate, residual=torch.ones_like(y[part]), device=DEV)
+            assert_close(y[part], ref, slack, f"{size} from row {first}")

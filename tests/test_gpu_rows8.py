@@ -147,6 +147,17 @@ def test_rows_of_zeros_nans_and_infinities(dtype, C):
     assert dvdq.rms_norm(x, None, eps=0.0)[1].isnan().all()                  # 0 / 0
 
 
+@pytest.mark.parametrize("act", [dvdq.ACT_SILU, dvdq.ACT_GELU_TANH, dvdq.ACT_GELU])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_infinities_and_the_largest_values_in_front_of_an_activation(dtype, act):
+    g = gen(12)
+    x, big = tensor(g, 4, 300, dtype=dtype), torch.finfo(dtype).max
+    x[0, 7], x[1, 8], x[2, 9], x[3, 10] = float("inf"), -float("inf"), -big, big
+    codes, scale = dvdq.quant8(x, act=act)
+    assert scale[:2].isnan().all() and not codes[:2].any()
+    assert torch.isfinite(scale[2:]).all() and int(codes[2, 9]) == 0 and codes[2].any() and int(codes[3, 10]) == 127 and int(codes[3].count_nonzero()) == 1
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_small_and_large_values(dtype):
     """Products that fp32 holds with few digits, and rows whose largest value is far above the others."""
