@@ -683,10 +683,10 @@ struct LinearPlan { int shape, splits, slices, group_n; size_t parts_bytes, pad_
 // and 1 to 12 parts: the choice takes 2 % longer than the best of them in the mean, 13 % at most; always 128 x 128 without parts
 // 35 % in the mean, 6.2 times at most.  8-bit codes, whose slices have as many bytes and matrix instructions: at 15 sizes 4 % longer than the best in the mean,
 // 15 % at most (17 x 13824 x 5120, 600 x 4608 x 1536).
-// Through registers: 16-bit products, 1.7 times that.  8-bit ones, a slice alone 0.3 us and 1.2 per 64 KB, or 1.5 times the share of the loads: of 15 sizes
-// with rows that are no whole pieces (40 to 50000 tokens, 100 to 12000 channels, K 88 to 9001) the choice, copies among it, takes 0.4 % longer than
-// the best of them in the mean, 5 % at most.  us, 128 x 128 tiles, 64 x 64, copied: 6242 x 1160 x 1156 20.5, 30.2, 26.4; 188 x 1720 x 1376 17.9, 13.8
-// (11.3 in parts), 14.1; 40 x 9001 x 1000 93, 62 (15.8 in parts), 20.1; 50000 x 777 x 100 20.9, 30.9, 30.9; 22268 x 4824 x 752 161, 215, 125;
+// Through registers: 16-bit products, 1.7 times that.  8-bit ones, a slice alone 0.3 us and 1.2 per 64 KB, or 1.4 times the share of the loads: of 18 sizes
+// with rows that are no whole pieces (40 to 50000 tokens, 100 to 12000 channels, K 88 to 9001) the choice, copies among it, takes 1.3 % longer than
+// the best in the mean, 6 % at most (256 x 128 and 128 x 64 tiles are faster by that where they are at all).  us, 128 x 128 tiles, 64 x 64, copied:
+// 6242 x 1160 x 1156 20.5, 30.2, 26.4; 188 x 1720 x 1376 17.9, 13.8 (11.3 in parts), 14.1; 3000 x 1000 x 1500 16.9, 22.3, 19.0; 40 x 9001 x 1000 93, 62 (15.8 in parts), 20.1; 50000 x 777 x 100 20.9, 30.9, 30.9; 22268 x 4824 x 752 161, 215, 125;
 // 10000 x 5000 x 5120 362, 544, 279.
 // K: bytes of a row; codes: 8-bit ones
 inline LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any, bool codes) {
@@ -706,7 +706,7 @@ inline LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool any, bool co
             const int64_t items = tiles * splits, full = items / slots;
             const int rest = (int)(items - full * slots);
             const bool held = any && codes;                  // (on the way to LDS in registers)
-            const float load = bytes * (lines ? 1.0f : 1.15f) * (held ? 1.5f : 1.0f) * (1 / 275e3f + (items < 256 ? (float)items / 256 : 1.0f) / 100e3f);
+            const float load = bytes * (lines ? 1.0f : 1.15f) * (held ? 1.4f : 1.0f) * (1 / 275e3f + (items < 256 ? (float)items / 256 : 1.0f) / 100e3f);
             const float lone = held ? 0.3f + 1.2f / 65536 * bytes : 0.34f + (lines ? 0.23f : 0.43f) / 65536 * bytes;
             auto round = [&](int resident) {
                 return 1.6f + (0.4f * (float)resident + (sh.per_cu == 1 ? 5.7f : 0.0f)) * area +
