@@ -500,8 +500,8 @@ int launch_held(const RowArgs &a, hipStream_t stream) {
     if constexpr (E::kVec == 8) {
         if (pieces <= 4096) return launch(integral_constant<int, 1024>(), integral_constant<int, 4>());
     } else {
-        if (pieces <= 3072) return launch(integral_constant<int, 512>(), integral_constant<int, 6>());
-        if (pieces <= 4096) return launch(integral_constant<int, 512>(), integral_constant<int, 8>());
+        if (pieces <= 6 * 512) return launch(integral_constant<int, 512>(), integral_constant<int, 6>());
+        if (pieces <= 8 * 512) return launch(integral_constant<int, 512>(), integral_constant<int, 8>());
     }
     row_long<E, MODE><<<dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), 1024, 0, stream>>>(a);
     return check_launch();
