@@ -244,8 +244,8 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
                 if (res)
 #pragma unroll
                     for (int j = 0; j < B; ++j) {
-                        const uint32_t up = max(m0 + 16 * (j0 + j) + row - (a.M - 1), 0);   // (tokens past the last read the last one's)
-                        r[j] = Row8::load(bytes_on(res + 16 * (j0 + j) * a.ldr + 32 * h, off_r) - up * a.ldr, count);
+                        const int from = min(16 * (j0 + j) + row, a.M - 1 - m0);   // tokens past the last read the last one's.  In 64 bits: one token's pitch may be anything
+                        r[j] = Row8::load(res + from * a.ldr + 32 * h + col, count);
                     }
 #pragma unroll
                 for (int j = 0; j < B; ++j) {
