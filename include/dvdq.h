@@ -398,8 +398,9 @@ size_t dvdq_group_norm_workspace_bytes(int64_t B, int64_t S, int64_t C, int64_t 
  * dvdq_w4ax_gemm (act_bits = 8).
  *
  * Codes are whole numbers next to 127 z / max|z|, ties to the even one, max over the row: those of the real numbers z that the formulas give
- * (activations and products in more than fp32 where a value is next to the border between two codes).  A row of zeros has scale 0.  A
- * row that holds a NaN or an infinity (z beyond fp32 counts as one) has codes 0 and scale NaN, so that its products are NaN.
+ * (activations and products in 64 bits where a value is next to the border between two codes, or fp32 has lost it: what is below 2^-1022 there
+ * counts as zero).  A row of zeros has scale 0.  A row that holds a NaN or an infinity (z beyond fp32 counts as one) has codes 0 and scale NaN,
+ * so that its products are NaN.
  */
 
 /*

@@ -108,6 +108,9 @@ struct Row {
 // An activation is good to 2^-18 of itself up to where it has fallen to 7.5e-5 (e^-12 times an argument of 12; see activate); beyond, it is that small.
 constexpr float kGood = 0x1p-18f, kFallen = 7.5e-5f;
 constexpr float kTiny = 0x1p-60f;                    // below, products in fp32 may have lost digits
+// An activation below 2^-118 may come out as zero (see activate).  Where the largest of a thread's factors times that is 2^-9 of the row's largest |z|
+// (1/4 of a code) or more, fp32 does not know the thread's elements, and all of them are worked out in 64 bits.
+static __device__ __forceinline__ bool lost_digits(float up_top, float top) { return up_top * 0x1p-118f > top * 0x1p-9f; }
 constexpr float kNearTop = 1.0f - 0x1p-13f;          // what may turn out to be the largest, as a share of the largest in fp32
 
 // Reductions over the T threads of a row (8 to 1024); every thread gets the result.  Beyond a wave through LDS, whose two halves take turns (`turn`).
@@ -293,10 +296,11 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
         return (l + T * (bit / V)) * V + bit % V;
     };
     Scale s = scale_from(over_row<T>(__builtin_bit_cast(uint32_t, top) & 0x7FFFFFFFu, Larger(), lds, turn));   // (a NaN's bits are above infinity's)
+    const bool wide = s.tiny || (MODE == kQuantAct && lost_digits(up_top, (float)s.top));   // (up_top is 0 where there is no factor)
     if (!r.exact || s.tiny) {
         double t = 0.0;
         if (s.fine) {
-            const float near = s.tiny ? 0.0f : (float)s.top * kNearTop;
+            const float near = wide ? 0.0f : (float)s.top * kNearTop;
             Mask which = 0;
             if (top >= near)
 #pragma unroll
@@ -341,14 +345,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_held(RowArgs a) {
     }
     // (a part that is not there is z = 0)
     const bool fallen = MODE == kQuantAct && (r.second ? up_top : 1.0f) * kFallen * s.reach > 0.25f;
-    if (s.fine && s.top > 0.0 && (s.tiny || fallen || far > 0.5f - (r.exact ? 0x1p-16f : 0x1p-15f))) {
+    if (s.fine && s.top > 0.0 && (wide || fallen || far > 0.5f - (r.exact ? 0x1p-16f : 0x1p-15f))) {
         Mask near = 0;
 #pragma unroll
         for (int i = 0; i < NP; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float t = z[i][e] * s.reach;
-                near |= (Mask)(s.tiny || fabsf(t - rintf(t)) > 0.5f - r.margin(t) ? 1 : 0) << (V * i + e);
+                near |= (Mask)(wide || fabsf(t - rintf(t)) > 0.5f - r.margin(t) ? 1 : 0) << (V * i + e);
             }
         for (; near; near &= near - 1) {
             const int c = place(near);
@@ -375,6 +379,7 @@ __global__ __launch_bounds__(1024) void row_long(RowArgs a) {
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const Row<E, MODE> r(a, (uint32_t)row);
+        float up_top = 0.0f;
         // the values and z of the n elements from c on, zero past them
         const auto piece = [&](int c, int n, float (&v)[V], float (&z)[V]) {
             const uint4 px = load_words<E>(r.x + c, n, true);
@@ -390,6 +395,7 @@ __global__ __launch_bounds__(1024) void row_long(RowArgs a) {
                 } else {
                     z[e] = MODE == kQuantAct ? act32(v[e], a.act) : v[e];
                     if (r.second) z[e] *= element<E>(ps, e);
+                    if (MODE == kQuantAct && r.second) up_top = fmaxf(up_top, fabsf(element<E>(ps, e)));
                 }
             }
         };
@@ -406,10 +412,12 @@ __global__ __launch_bounds__(1024) void row_long(RowArgs a) {
         float factor = 1.0f;
         if (is_norm(MODE)) factor = rsqrtf(fmaf(over_row<T>(sum, Add(), lds, turn), a.share, a.eps));
         Scale s = {};
+        bool wide = false;
         if (MODE != kNorm) {
             s = scale_from(over_row<T>(__builtin_bit_cast(uint32_t, top) & 0x7FFFFFFFu, Larger(), lds, turn));
+            wide = s.tiny || (MODE == kQuantAct && lost_digits(up_top, (float)s.top));
             if (!r.exact || s.tiny) {
-                const float near = s.tiny ? 0.0f : (float)s.top * kNearTop;
+                const float near = wide ? 0.0f : (float)s.top * kNearTop;
                 double t = 0.0;
                 if (s.fine && top >= near)
                     for (int c = threadIdx.x * V; c < a.C; c += T * V)
@@ -439,7 +447,7 @@ __global__ __launch_bounds__(1024) void row_long(RowArgs a) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const float t = z[e] * s.reach, q = rintf(t);
-                near |= (s.tiny || fabsf(t - q) > 0.5f - r.margin(t) ? 1u : 0u) << e;
+                near |= (wide || fabsf(t - q) > 0.5f - r.margin(t) ? 1u : 0u) << e;
                 o.e[e] = s.fine ? (int8_t)(int)q : 0;
                 total += o.e[e];
             }
