@@ -127,7 +127,6 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
     using E = typename P::Out;
     using Raw = typename E::Raw;
     using Row8 = Eight<E>;
-    constexpr int B = FM < 4 ? FM : 4;
     const Raw *bias_row = static_cast<const Raw *>(a.bias), *gate_rows = static_cast<const Raw *>(a.gate);
     const int lane = threadIdx.x & 63, row = lane & 15, col = 8 * (lane >> 4);
     if (m0 >= a.M || n0 >= a.N) return;
@@ -171,28 +170,58 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += p.at(i);
     };
-    if (m0 + 16 * FM <= a.M && n0 + 64 <= a.N && (!a.gate || shared_gate)) {
+    // The lane's row of the gate, token by token (16 apart): a division once, for the first
+    struct GateRow {
+        int q, left, first_q, first_left, by, by_left, tokens;
+        __device__ __forceinline__ GateRow(const LinearArgs &a, int m) : tokens(a.gate_rows) {
+            first_q = m / tokens, first_left = m - first_q * tokens;
+            by = 16 / tokens, by_left = 16 - by * tokens;
+        }
+        __device__ __forceinline__ void begin() {
+            q = first_q, left = first_left;
+            asm volatile("" : "+v"(q));   // (or the second half's addresses are the first's, kept in registers)
+        }
+        __device__ __forceinline__ int next() {
+            const int here = q;
+            left += by_left;
+            q += by + (left >= tokens ? 1 : 0);
+            left -= left >= tokens ? tokens : 0;
+            return here;
+        }
+    };
+    if (m0 + 16 * FM <= a.M && n0 + 64 <= a.N) {
         // Loads come back behind the stores in front of them, and behind a branch around a load the compiler waits for all of both.  So each
         // combination of gate and residual has its own way without branches, and what the next chunk of B tokens is made of is requested before the
-        // stores of the present one, the residual (which y may be: the compiler could not move its loads above a store) two chunks ahead.
+        // stores of the present one, the residual (which y may be: the compiler could not move its loads above a store) two chunks ahead, and
+        // with it the gate where tokens have rows of their own (as edge tiles have it, token by token behind the stores, 32760 x 1536 x 1536 with a
+        // residual took 201 us in place of 174, 8011 x 9621 x 293 208 in place of 161, 6240 x 1536 x 1536 51.5 in place of 43.2).
         const auto whole = [&](auto gated, auto added) {
-            constexpr bool GATE = decltype(gated)::value, RES = decltype(added)::value;
-            constexpr int C = FM / B;                        // chunks of 32 channels
+            constexpr int GATE = decltype(gated)::value;     // 1: one row for all tokens, 2: rows of their own
+            constexpr bool RES = decltype(added)::value, AHEAD = RES || GATE == 2;
+            constexpr int B = std::min(FM, GATE < 2 ? 4 : FM == 8 ? 1 : sizeof(Raw) == 4 ? 2 : 4), C = FM / B;   // tokens of a chunk, as registers allow; chunks of 32 channels
             Scales s;
-            Row8 bias, gate, r[2][B], out[B];
+            Row8 bias, gate, r[2][RES ? B : 1], g[2][GATE == 2 ? B : 1], out[B];
             auto vectors = [&](int h) {
                 const int n = n0 + 32 * h + col;
                 s = scales(n, 8);
                 bias = Row8();
                 if (a.bias) bias = Row8::load(bias_row + n, 8);
-                if constexpr (GATE) gate = Row8::load(gate_rows + (m0 / a.gate_rows) * a.ldg + n, 8);
+                if constexpr (GATE == 1) gate = Row8::load(gate_rows + (m0 / a.gate_rows) * a.ldg + n, 8);
             };
+            GateRow gate_row(a, m0 + row);
             auto fetch = [&](int c) {
+                if constexpr (RES) {
 #pragma unroll
-                for (int j = 0; j < B; ++j) r[c & 1][j] = Row8::load(bytes_on(res + 16 * (c % C * B + j) * a.ldr + 32 * (c / C), off_r), 8);
+                    for (int j = 0; j < B; ++j) r[c & 1][j] = Row8::load(bytes_on(res + 16 * (c % C * B + j) * a.ldr + 32 * (c / C), off_r), 8);
+                }
+                if constexpr (GATE == 2) {
+                    if (c % C == 0) gate_row.begin();
+#pragma unroll
+                    for (int j = 0; j < B; ++j) g[c & 1][j] = Row8::load(gate_rows + gate_row.next() * a.ldg + (n0 + 32 * (c / C) + col), 8);
+                }
             };
             vectors(0);
-            if constexpr (RES) {
+            if constexpr (AHEAD) {
                 fetch(0);
                 fetch(1);
             }
@@ -203,13 +232,14 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
                 for (int j = 0; j < B; ++j) {
                     float v[8];
                     values(v, h, j0 + j, bias, s);
-                    if constexpr (GATE) times(v, gate);
+                    if constexpr (GATE == 1) times(v, gate);
+                    if constexpr (GATE == 2) times(v, g[c & 1][j]);
                     if constexpr (RES) plus(v, r[c & 1][j]);
                     out[j] = Row8::rounded(v);
                     __builtin_amdgcn_sched_barrier(0);
                 }
                 if (c == C - 1) vectors(1);
-                if constexpr (RES)
+                if constexpr (AHEAD)
                     if (c + 2 < 2 * C) fetch(c + 2);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -221,16 +251,17 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-        using std::true_type;
-        using std::false_type;
-        if (a.gate) {
-            if (res) whole(true_type(), true_type());
-            else whole(true_type(), false_type());
-        } else {
-            if (res) whole(false_type(), true_type());
-            else whole(false_type(), false_type());
-        }
+        const auto gated = [&](auto which) {
+            if (res) whole(which, std::true_type());
+            else whole(which, std::false_type());
+        };
+        if (!a.gate) gated(std::integral_constant<int, 0>());
+        else if (shared_gate) gated(std::integral_constant<int, 1>());
+        else gated(std::integral_constant<int, 2>());
     } else {
+        constexpr int B = FM == 8 ? 2 : FM;
+        GateRow gate_row(a, m0 + row);
+        const int last_row = (a.M - 1) / a.gate_rows;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int n = n0 + 32 * h + col, count = min(8, a.N - n);
@@ -238,9 +269,13 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
             const Scales s = scales(n, count);
             Row8 bias = {};
             if (a.bias) bias = Row8::load(bias_row + n, count);
+            gate_row.begin();
 #pragma unroll
             for (int j0 = 0; j0 < FM; j0 += B) {
-                Row8 r[B] = {};
+                Row8 r[B] = {}, g[B] = {};
+                if (a.gate)
+#pragma unroll
+                    for (int j = 0; j < B; ++j) g[j] = Row8::load(gate_rows + min(gate_row.next(), last_row) * a.ldg + n, count);
                 if (res)
 #pragma unroll
                     for (int j = 0; j < B; ++j) {
@@ -253,7 +288,7 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
                     if (m < a.M) {
                         float v[8];
                         values(v, h, j0 + j, bias, s);
-                        if (a.gate) times(v, Row8::load(gate_rows + (m / a.gate_rows) * a.ldg + n, count));
+                        if (a.gate) times(v, g[j]);
                         if (res) plus(v, r[j]);
                         store_piece<E, 8>(bytes_on(y + 16 * (j0 + j) * a.ldy + 32 * h, off_y), Row8::rounded(v).piece(), count);
                     }
