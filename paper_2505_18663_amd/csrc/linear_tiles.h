@@ -544,9 +544,9 @@ static __device__ __forceinline__ void lds_direct_load16_at(const void *p, uint3
 __device__ uint4 zero_piece;   // what the pieces past K of the last slice are read from
 
 // Tiles of 64 WN channels x 16 FM WM tokens, WN x WM waves of 64 channels x 16 FM tokens each; slices of 128 bytes of K.
-// Tokens have three slices in LDS, weights two: while a slice is multiplied, the next is there, the tokens of the one after it
-// come in, and its weights follow as soon as those of the present slice have been read.  (The tokens are what comes from further away: with three
-// slices of weights and two of tokens 8-bit 32760 x 13824 x 5120 took 1734 to 1810 us in place of 1693 to 1757, 32760 x 8960 x 1536 360 in place of 351.
+// Tokens have three slices in LDS, weights two, or the other way round (slices_of_weights): while a slice is multiplied, the next is there, the tokens of
+// the one after it come in, and its weights follow as soon as those of the present slice have been read.  (The tokens are what comes from further away: with three
+// slices of weights and two of tokens, 256 x 256 tiles, 8-bit 32760 x 13824 x 5120 took 1734 to 1810 us in place of 1693 to 1757, 32760 x 8960 x 1536 360 in place of 351.
 // What bounds the loop on a full chip is the way from the L2s into LDS, 54 to 69 GB/s per compute unit where 32 of them share panels; it must not run dry.
 // Five slices of tokens and four of weights for 128 x 128 and smaller tiles: 8-bit 600 x 4608 x 1536 20.1 -> 16.0 us, 17 x 13824 x 5120 23.7 -> 20.3, 1000 x 8960 x 1536
 // 28.1 -> 25.6, but 1560 x 1536 x 1536 11.3 -> 11.9, 512 x 4096 x 5120 level, and one workgroup a compute unit; not kept.)
@@ -555,13 +555,18 @@ __device__ uint4 zero_piece;   // what the pieces past K of the last slice are r
 // in LDS for every wave, and this one's place is free.
 // A workgroup takes tile after tile, without a seam: the last slices of a tile load the first ones of the next, which is multiplied
 // while the outputs are still being written.
+// 256 channels x 128 tokens, two thirds of whose loads are weights: 886 x 6016 x 9984 106 to 114 -> 102 us, 1000 x 5120 x 5120 58.8 to 62 -> 56.7, 8-bit 57.4 -> 55.0 and
+// 34.3 -> 32.9.  128 x 64: level, 7212 x 1093 x 64 12.6 -> 13.5.
+constexpr int slices_of_weights(int BN, int BM) { return BN > 128 && BN > BM ? 3 : 2; }
 template <typename P, int ACT, int FM, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, int group_n) {
     constexpr int W = WN * WM, BN = 64 * WN, BM = 16 * FM * WM, FH = FM < 4 ? FM : 4, NH = FM / FH, PH = 2 * NH;
     constexpr int LW = BN / 8 / W, LX = BM / 8 / W;          // loads of a wave per slice, 8 rows each
+    constexpr int kAhead = slices_of_weights(BN, BM) == 3 ? LW : LX;   // of the operand that is loaded two slices ahead
     constexpr int kStores = ACT == kPart || sizeof(typename P::Out::Raw) == 4 ? 4 * FM : 2 * FM;   // of a wave per whole tile, at least
     constexpr uint32_t kUnitW = BN * 128, kUnitX = BM * 128;
-    extern __shared__ uint4 lds[];                           // weights: 2 units, tokens: 3
+    constexpr int SW = slices_of_weights(BN, BM), SX = 5 - SW;
+    extern __shared__ uint4 lds[];                           // weights: SW units, tokens: SX
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n_tiles = (a.N + BN - 1) / BN, m_tiles = (a.M + BM - 1) / BM, tiles = n_tiles * m_tiles, items = tiles * a.splits, grid = gridDim.x;
     const int wn = wave % WN * 64, wm = wave / WN * 16 * FM;
@@ -573,7 +578,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
     const int xcds = min(8, grid), xcd = blockIdx.x % xcds, step = (grid - xcd + xcds - 1) / xcds;
     const int share = items / xcds, more = items % xcds;     // (the first XCDs have one more, of workgroups as well as of tiles)
     const int end = share * (xcd + 1) + min(xcd + 1, more);
-    const uint32_t lds_w = lds_address(lds) + wave * (1024 * LW), lds_x = lds_address(lds) + 2 * kUnitW + wave * (1024 * LX);
+    const uint32_t lds_w = lds_address(lds) + wave * (1024 * LW), lds_x = lds_address(lds) + SW * kUnitW + wave * (1024 * LX);
     const uint8_t *src_w, *src_x;
     uint32_t off_w[LW], off_x[LX];
     const bool spread_w = a.N * a.ldw < (int64_t)1 << 32, spread_x = a.M * a.ldx < (int64_t)1 << 32;   // offsets of 32 bits
@@ -633,7 +638,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
     // fragment reads: LDS row r of 128 bytes holds its 16-byte piece c at c ^ ((r >> 1) & 7), so that the 16 rows that a read takes at
     // once lie in different banks
     const int at = (lane & 15) * 8 + ((lane >> 4) ^ ((lane & 15) >> 1));   // of k-step 0; k-step 1 is piece ^ 4
-    const int at_w = wn * 8 + at, at_x = 2 * (kUnitW / 16) + wm * 8 + at;
+    const int at_w = wn * 8 + at, at_x = SW * (kUnitW / 16) + wm * 8 + at;
     typename P::Acc acc[4][FM] = {};
     uint4 fw[2][4], fx[2][FH];
     auto read = [&](int sw, int sx, int p) {                 // the fragments of phase p of the slice in these places
@@ -661,7 +666,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
         // STEADY: slices of this tile follow, all within K
         auto slice = [&](int q, auto steady) {
             constexpr bool STEADY = decltype(steady)::value;
-            const int nx = sx == 2 ? 0 : sx + 1, ax = nx == 2 ? 0 : nx + 1;
+            const int nw = sw == SW - 1 ? 0 : sw + 1, nx = sx == SX - 1 ? 0 : sx + 1;   // of the next slice
             bool loads = true;                               // what is loaded two slices ahead
             int lq = q + 2;
             if (!STEADY && lq >= slices) {
@@ -673,14 +678,20 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
             for (int p = 0; p < PH; ++p) {
                 if (p < PH - 1) {
                     read(sw, sx, p + 1);
-                    if (p == 0 && loads) load_x(lq, ax, STEADY);
+                    if (p == 0 && loads) {
+                        if constexpr (SW == 3) load_w(lq, nw == 2 ? 0 : nw + 1, STEADY);
+                        else load_x(lq, nx == 2 ? 0 : nx + 1, STEADY);
+                    }
                 } else if (STEADY || q + 1 < slices || next < end) {
                     if (!STEADY && !loads) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                    else if (STEADY || !(stored && q == 0)) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LX) : "memory");
-                    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LX + kStores) : "memory");
+                    else if (STEADY || !(stored && q == 0)) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kAhead + kStores) : "memory");
                     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                    if (loads) load_w(lq, sw, STEADY);
-                    if (STEADY || q + 1 < slices) read(sw ^ 1, nx, 0);   // (of the next tile: behind the outputs)
+                    if (loads) {
+                        if constexpr (SW == 3) load_x(lq, sx, STEADY);
+                        else load_w(lq, sw, STEADY);
+                    }
+                    if (STEADY || q + 1 < slices) read(nw, nx, 0);   // (of the next tile: behind the outputs)
                 }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -689,8 +700,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
                     for (int j = 0; j < FH; ++j) acc[i][(p % NH) * FH + j] = P::mfma(fw[p / NH][i], fx[p & 1][j], acc[i][(p % NH) * FH + j]);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            sw = nw;
             sx = nx;
-            sw ^= 1;
         };
         const int steady = stored ? 1 : 0;
 #pragma unroll 1
@@ -715,7 +726,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, in
 template <typename P, int ACT, int FM, int WN, int WM>
 int launch_tiles(const LinearArgs &a, int per_cu, int group_n, hipStream_t stream) {
     constexpr int BN = 64 * WN, BM = 16 * FM * WM;
-    constexpr size_t kLds = (2 * BN + 3 * BM) * 128;
+    constexpr int SW = slices_of_weights(BN, BM);
+    constexpr size_t kLds = (SW * BN + (5 - SW) * BM) * 128;
     static std::atomic<uint64_t> done{0};
     const auto kernel = linear_tiles<P, ACT, FM, WN, WM>;
     allow_dynamic_lds(reinterpret_cast<const void *>(kernel), kLds, done);
