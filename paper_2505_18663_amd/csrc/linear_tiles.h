@@ -199,7 +199,9 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
         const auto whole = [&](auto gated, auto added) {
             constexpr int GATE = decltype(gated)::value;     // 1: one row for all tokens, 2: rows of their own
             constexpr bool RES = decltype(added)::value, AHEAD = RES || GATE == 2;
-            constexpr int B = std::min(FM, GATE < 2 ? 4 : FM == 8 ? 1 : sizeof(Raw) == 4 ? 2 : 4), C = FM / B;   // tokens of a chunk, as registers allow; chunks of 32 channels
+            // As many tokens as registers hold: with four of 256 x 256 tiles' 8-bit ones, 29 to 105 words spilt, 118800 x 1536 x 1536 with gate and residual 407 us in
+            // place of 367, 32760 x 13824 x 5120 2150 and 2065, fp32 outputs 32760 x 5120 x 1536 592 and 498.
+            constexpr int B = std::min(FM, GATE < 2 ? (FM == 8 && P::kScaled ? 2 : 4) : FM == 8 ? 1 : sizeof(Raw) == 4 ? 2 : 4), C = FM / B;   // tokens of a chunk, chunks of 32 channels
             Scales s;
             Row8 bias, gate, r[2][RES ? B : 1], g[2][GATE == 2 ? B : 1], out[B];
             auto vectors = [&](int h) {
