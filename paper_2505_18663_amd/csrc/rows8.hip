@@ -151,7 +151,7 @@ struct Scale {
     bool fine, tiny; // no NaN or infinity; products may have lost digits
 };
 static __device__ __forceinline__ float scale_of(const Scale &s, float factor) {
-    return !s.fine ? __builtin_nanf("") : s.top > 0.0 ? (float)s.top * (1.0f / 127.0f) * factor : 0.0f;
+    return !s.fine ? __builtin_nanf("") : s.top > 0.0 ? (float)(s.top * (1.0 / 127.0) * factor) : 0.0f;   // one rounding
 }
 static __device__ __forceinline__ Scale scale_from(uint32_t top_bits) {
     const float top = __builtin_bit_cast(float, top_bits);
