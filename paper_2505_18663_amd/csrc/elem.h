@@ -1,4 +1,4 @@
-// Element types of the operators around the quantized layer (rope.hip, group_norm.hip, linear16.hip): conversions to and from
+// Element types of the operators around the quantized layer (rope.hip, group_norm.hip, rows8.hip, linear_tiles.h): conversions to and from
 // fp32, 16-byte pieces of a row at any element's address, activations.
 #pragma once
 #include <type_traits>

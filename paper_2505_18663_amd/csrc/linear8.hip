@@ -5,9 +5,9 @@
 // Products on the INT8 matrix cores, summed exactly in int32; scales and epilogue in fp32, one rounding to the tensors' type.  The kernels
 // are those of linear_tiles.h: 128 bytes of a row are a slice, whatever the type, and a matrix instruction takes as long for them.
 //
-// us, with what the library's int8 product takes (int32 outputs, no scales, no epilogue): 32760 x 13824 x 5120 with gate and residual 1690 to 1750 and 1750 to 1870,
-// 32760 x 1536 x 8960 with tanh GELU 461 to 480 and 512 to 520, 8192^3 409 and 441, 512 x 4096 x 5120 with tanh GELU 21 and 20 to 23, 1560 x 1536 x 1536 11 and 19,
-// 6242 x 1168 x 1160 19 and 35, 64 x 5120 x 5120 14.5 and 18, 2 x 1536 x 9216 5.8.  2.65 to 2.74 POP/s where K is large: the way from the L2s into LDS and the power
+// us, with what the library's int8 product takes (int32 outputs, no scales, no epilogue): 32760 x 13824 x 5120 with gate and residual 1670 to 1735 and 1750 to 1870,
+// 32760 x 1536 x 8960 with tanh GELU 461 to 484 and 512 to 520, 8192^3 409 and 441, 512 x 4096 x 5120 with tanh GELU 21 and 20 to 23, 1560 x 1536 x 1536 11 and 19,
+// 6242 x 1168 x 1160 19 and 35, 64 x 5120 x 5120 14 and 18, 2 x 1536 x 9216 5.6.  2.67 to 2.77 POP/s where K is large: the way from the L2s into LDS and the power
 // limit (1.93 GHz); outputs of short K wait for the acknowledgement of the stores in front of the next tile's loads (9 us a tile beside 1.6 us a slice).
 #include "linear_tiles.h"
 
@@ -29,8 +29,8 @@ int launch_linear8(const int8_t *codes, int64_t ldc, const float *x_scale, const
     return with_type(dtype, [&](auto type) {
         using E = decltype(type);
         // A lane's 8 fp32 outputs are two stores of 16 bytes with a gap between those of the token's lanes, which caches fill and stores past them do
-        // not: 8192 x 8192 x 1024 137 us past them, 98 through them, 32760 x 1536 x 1536 114 and 94, x 8960 365 and 360.  Where outputs and residual are more than
-        // the last cache, 256 MB, it is the other way round: 32760 x 1536 x 1536 with a residual 148 and 157, 32760 x 13824 x 5120 2386 and 2438, 118800 x 1536 x 1536
+        // not: 8192 x 1024 x 8192 137 us past them, 98 through them, 32760 x 1536 x 1536 114 and 94, 32760 x 8960 x 1536 365 and 360.  Where outputs and residual are more than
+        // the last cache, 256 MB, it is the other way round: 32760 x 1536 x 1536 with a residual 148 and 157, 32760 x 5120 x 13824 2386 and 2438, 118800 x 1536 x 1536
         // without one 343 and 352.
         constexpr bool WIDE = sizeof(typename E::Raw) == 4;
         a.streaming = (WIDE ? M * N * (residual ? 2 : 1) > (64 << 20) : M * N >= (2 << 20)) && ldy * sizeof(typename E::Raw) % 64 == 0 && (reinterpret_cast<uintptr_t>(y) & 63) == 0;

@@ -65,7 +65,8 @@ struct LinearArgs {
     float4 *parts;                     // sums of parts of K, in the order of the accumulators (kPart)
     int splits, slices;                // parts of K; slices of 128 bytes of a part
     // Outputs past the caches, where they are larger than an XCD's L2 and the 64 bytes that the lanes of a token write are sectors of their own
-    // (rows and address multiples of 64 bytes): 32760 x 1536 x 8960 with tanh GELU 823 -> 775 us, 32760 x 1536 x 4608 395 -> 364, 118800 x 1536 x 1536 513 -> 510.
+    // (rows and address multiples of 64 bytes): 32760 x 1536 x 8960 with tanh GELU 823 -> 775 us, 32760 x 1536 x 4608 395 -> 364, 118800 x 1536 x 1536 513 -> 510.  (fp32
+    // outputs: see launch_linear8.)
     bool streaming;
 };
 constexpr int kPart = 4;               // in the place of an activation: leave the sums of a part of K for linear_join
@@ -195,12 +196,12 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
         // combination of gate and residual has its own way without branches, and what the next chunk of B tokens is made of is requested before the
         // stores of the present one, the residual (which y may be: the compiler could not move its loads above a store) two chunks ahead, and
         // with it the gate where tokens have rows of their own (as edge tiles have it, token by token behind the stores, 32760 x 1536 x 1536 with a
-        // residual took 201 us in place of 174, 8011 x 9621 x 293 208 in place of 161, 6240 x 1536 x 1536 51.5 in place of 43.2).
+        // residual took 201 us in place of 174, 8011 x 293 x 9621 208 in place of 161, 6240 x 1536 x 1536 51.5 in place of 43.2).
         const auto whole = [&](auto gated, auto added) {
             constexpr int GATE = decltype(gated)::value;     // 1: one row for all tokens, 2: rows of their own
             constexpr bool RES = decltype(added)::value, AHEAD = RES || GATE == 2;
             // As many tokens as registers hold: with four of 256 x 256 tiles' 8-bit ones, 29 to 105 words spilt, 118800 x 1536 x 1536 with gate and residual 407 us in
-            // place of 367, 32760 x 13824 x 5120 2150 and 2065, fp32 outputs 32760 x 5120 x 1536 592 and 498.
+            // place of 367, 32760 x 5120 x 13824 2150 and 2065, fp32 outputs 32760 x 1536 x 5120 592 and 498.
             constexpr int B = std::min(FM, GATE < 2 ? (FM == 8 && P::kScaled ? 2 : 4) : FM == 8 ? 1 : sizeof(Raw) == 4 ? 2 : 4), C = FM / B;   // tokens of a chunk, chunks of 32 channels
             Scales s;
             Row8 bias, gate, r[2][RES ? B : 1], g[2][GATE == 2 ? B : 1], out[B];
@@ -264,7 +265,7 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
     } else {
         constexpr int B = FM == 8 ? 2 : FM;
         // WHOLE: the lanes have 8 channels or none.  (Code that is run once takes longer to fetch than to run: without that for parts of 8 channels
-        // 500 x 512 x 131 8.6 -> 7.7 us, 2559 x 160 x 87 6.7 -> 5.8.)
+        // 500 x 131 x 512 8.6 -> 7.7 us, 2559 x 87 x 160 6.7 -> 5.8.)
         const auto edge = [&](auto whole_pieces) {
             constexpr bool WHOLE = decltype(whole_pieces)::value;
 #pragma unroll
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_any(LinearArgs a, int 
     extern __shared__ uint4 lds[];                           // two slices of BN rows of weights, BM of tokens
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n_tiles = (a.N + BN - 1) / BN, m_tiles = (a.M + BM - 1) / BM, tiles = n_tiles * m_tiles, grid = gridDim.x;
-    // A run of tiles for each XCD, as there.  (Divisions that a launch can do without are left out: 512 x 512 x 131 8.1 -> 7.9 us.)
+    // A run of tiles for each XCD, as there.  (Divisions that a launch can do without are left out: 512 x 131 x 512 8.1 -> 7.9 us.)
     const int xcd = blockIdx.x & 7, t = (grid >> 3) * xcd + min(xcd, grid & 7) + (blockIdx.x >> 3), split = a.splits == 1 ? 0 : t / tiles;
     int m0, n0;
     if (group_n >= n_tiles) {
@@ -348,7 +349,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void linear_any(LinearArgs a, int 
     const int piece = tid & 7, row0 = tid >> 3;
     uint4 pw[LW], px[LX];
     // Of a slice across the rows' end a thread loads the 16 bytes that end with the row, in the place of its piece or of one past the end, and shifts
-    // them on their way to LDS: as pieces that hang on conditions, each load was waited for (40 x 1536 x 100 7.2 -> 6.8 us).
+    // them on their way to LDS: as pieces that hang on conditions, each load was waited for (40 x 100 x 1536 7.2 -> 6.8 us).
     auto load = [&](int q) __attribute__((always_inline)) {
         const auto rows = [&](int from, int count) __attribute__((always_inline)) {
 #pragma unroll
@@ -557,8 +558,8 @@ __device__ uint4 zero_piece;   // what the pieces past K of the last slice are r
 // in LDS for every wave, and this one's place is free.
 // A workgroup takes tile after tile, without a seam: the last slices of a tile load the first ones of the next, which is multiplied
 // while the outputs are still being written.
-// 256 channels x 128 tokens, two thirds of whose loads are weights: 886 x 6016 x 9984 106 to 114 -> 102 us, 1000 x 5120 x 5120 58.8 to 62 -> 56.7, 8-bit 57.4 -> 55.0 and
-// 34.3 -> 32.9.  128 x 64: level, 7212 x 1093 x 64 12.6 -> 13.5.
+// 256 channels x 128 tokens, two thirds of whose loads are weights: 886 x 9984 x 6016 106 to 114 -> 102 us, 1000 x 5120 x 5120 58.8 to 62 -> 56.7, 8-bit 57.4 -> 55.0 and
+// 34.3 -> 32.9.  128 x 64: level, 7212 x 64 x 1093 12.6 -> 13.5.
 constexpr int slices_of_weights(int BN, int BM) { return BN > 128 && BN > BM ? 3 : 2; }
 template <typename P, int ACT, int FM, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, int group_n) {

@@ -59,3 +59,13 @@ def test_the_last_token_of_a_clip():
     last = hidden[:, -1]
     assert last.stride(0) == 32760 * 5120
     assert torch.equal(dvdq.linear(x, w, residual=last), dvdq.linear(x, w, residual=last.clone()))
+
+
+@pytest.mark.parametrize("M,K", [(1, 4104), (40, 264), (300, 260), (200, 4099)])
+def test_one_channel_of_any_pitch(M, K):
+    """The same of weights that are one row."""
+    g = torch.Generator(device=DEV).manual_seed(M)
+    x, w = (torch.randn((n, K), generator=g, device=DEV).bfloat16() for n in (M, 1))
+    want = dvdq.linear(x, w)
+    for pitch in PITCHES:
+        assert torch.equal(dvdq.linear(x, lay(w, pitch)), want), pitch
