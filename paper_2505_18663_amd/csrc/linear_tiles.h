@@ -304,7 +304,7 @@ static __device__ __forceinline__ void epilogue(const LinearArgs &a, const typen
                 }
             }
         };
-        if (FM < 8 && a.N % 8 == 0) edge(std::true_type());
+        if (FM < 8 && (a.N % 8 == 0 || n0 + 64 <= a.N)) edge(std::true_type());
         else edge(std::false_type());
     }
 }
