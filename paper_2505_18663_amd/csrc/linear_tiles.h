@@ -558,9 +558,10 @@ __device__ uint4 zero_piece;   // what the pieces past K of the last slice are r
 // in LDS for every wave, and this one's place is free.
 // A workgroup takes tile after tile, without a seam: the last slices of a tile load the first ones of the next, which is multiplied
 // while the outputs are still being written.
-// 256 channels x 128 tokens, two thirds of whose loads are weights: 886 x 9984 x 6016 106 to 114 -> 102 us, 1000 x 5120 x 5120 58.8 to 62 -> 56.7, 8-bit 57.4 -> 55.0 and
-// 34.3 -> 32.9.  128 x 64: level, 7212 x 64 x 1093 12.6 -> 13.5.
-constexpr int slices_of_weights(int BN, int BM) { return BN > 128 && BN > BM ? 3 : 2; }
+// Tiles of 256 x 128 and 128 x 64, two thirds of whose loads are weights: 886 x 9984 x 6016 106 to 114 -> 102 us, 1000 x 5120 x 5120 58.8 to 62 -> 56.7, 8-bit 57.4 -> 55.0 and
+// 34.3 -> 32.9; where rows are no whole lines 2 x 7592 x 3080 18.0 -> 16.2, 33 x 5000 x 5000 19.2 -> 17.5, 8-bit 40 x 7600 x 3080 14.2 -> 13.5; but 7212 x 64 x 1093
+// 12.5 -> 13.5, 8-bit 17 x 5120 x 13824 19.2 -> 20.1.
+constexpr int slices_of_weights(int BN, int BM) { return BN > BM ? 3 : 2; }
 template <typename P, int ACT, int FM, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, 2) void linear_tiles(LinearArgs a, int group_n) {
     constexpr int W = WN * WM, BN = 64 * WN, BM = 16 * FM * WM, FH = FM < 4 ? FM : 4, NH = FM / FH, PH = 2 * NH;
