@@ -5,8 +5,8 @@
 // Products on the matrix cores, sums and epilogue in fp32, one rounding to the tensors' type.
 //
 // The kernels are those of linear_tiles.h.  Against the library's product of the card's torch, which has no
-// epilogue, weights out of the caches: 32760 x 13824 x 5120 with a residual 3170 to 3305 us and 2920 to 3120, 32760 x 1536 x 8960
-// with tanh GELU 740 to 790 and 660 to 750, 512 x 4096 x 5120 33 to 37 and 36 to 38, 64 x 5120 x 5120 20 and 22, 1560 x 1536 x 1536 17 and 20, 2 x 1536 x 9216
+// epilogue, weights out of the caches: 32760 x 13824 x 5120 with a residual 3170 to 3367 us and 2920 to 3120, 32760 x 1536 x 8960
+// with tanh GELU 740 to 807 and 660 to 750, 512 x 4096 x 5120 33 to 37 and 36 to 38, 64 x 5120 x 5120 20 and 22, 1560 x 1536 x 1536 17 and 20, 2 x 1536 x 9216
 // 8.4 to 9.1 and 20, 32760 x 1533 x 8960 740 to 780 and 890 to 910.
 #include "linear_tiles.h"
 

@@ -6,9 +6,9 @@
 // are those of linear_tiles.h: 128 bytes of a row are a slice, whatever the type, and a matrix instruction takes as long for them.
 //
 // us, with what the library's int8 product takes (int32 outputs, no scales, no epilogue): 32760 x 13824 x 5120 with gate and residual 1670 to 1735 and 1750 to 1870,
-// 32760 x 1536 x 8960 with tanh GELU 461 to 484 and 512 to 520, 8192^3 409 and 441, 512 x 4096 x 5120 with tanh GELU 21 and 20 to 23, 1560 x 1536 x 1536 11 and 19,
+// 32760 x 1536 x 8960 with tanh GELU 464 to 470 and 512 to 520, 8192^3 409 and 441, 512 x 4096 x 5120 with tanh GELU 21 and 20 to 23, 1560 x 1536 x 1536 11 and 19,
 // 6242 x 1168 x 1160 19 and 35, 64 x 5120 x 5120 14 and 18, 2 x 1536 x 9216 5.6.  2.67 to 2.77 POP/s where K is large: the way from the L2s into LDS and the power
-// limit (1.93 GHz); outputs of short K wait for the acknowledgement of the stores in front of the next tile's loads (9 us a tile beside 1.6 us a slice).
+// limit (1.93 GHz); outputs of short K wait for the acknowledgement of the stores in front of the next tile's loads (8 us a tile beside 1.6 us a slice).
 #include "linear_tiles.h"
 
 namespace dvdq {
